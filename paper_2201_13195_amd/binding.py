@@ -8,6 +8,7 @@ does not take (and calls with event pairs) go through the ctypes functions here,
 checks say what is wrong with them."""
 import ctypes
 import os
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -35,6 +36,11 @@ class _State(ctypes.Structure):
 class _Desc(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int64), ("d_in", ctypes.c_int64), ("d_out", ctypes.c_int64), ("k", ctypes.c_int64),
                 ("dtype", ctypes.c_int32), ("kind", ctypes.c_int32)]
+
+
+class _Mat8(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64), ("scales", ctypes.c_void_p), ("ld_scales", ctypes.c_int64),
+                ("f8", ctypes.c_int32), ("scale", ctypes.c_int32)]
 
 
 def lib_path():
@@ -82,6 +88,19 @@ def load_library():
     L.rmm_probe_mfma.argtypes = [ci, ci, vp, vp]
     L.rmm_probe_read.restype = ci
     L.rmm_probe_read.argtypes = [vp, sz, ci, vp, vp]
+    mat = ctypes.POINTER(_Mat8)
+    L.rmm_quantize8.restype = ci
+    L.rmm_quantize8.argtypes = [i64, i64, ci, vp, mat, vp]
+    L.rmm_quantize8_weight.restype = ci
+    L.rmm_quantize8_weight.argtypes = [i64, i64, ci, vp, mat, mat, vp]
+    L.rmm_linear8.restype = ci
+    L.rmm_linear8.argtypes = [i64, i64, i64, ci, mat, mat, vp, vp, vp]
+    L.rmm_rms_norm.restype = ci
+    L.rmm_rms_norm.argtypes = [i64, i64, ci, ctypes.c_float, vp, vp, vp, vp, vp, mat, vp, vp]
+    L.rmm_rms_norm_workspace_bytes.restype = sz
+    L.rmm_rms_norm_workspace_bytes.argtypes = [i64, i64, ci]
+    L.rmm_rms_norm_backward.restype = ci
+    L.rmm_rms_norm_backward.argtypes = [i64, i64, ci, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.rmm_debug_philox.restype = ci
     L.rmm_debug_philox.argtypes = [_State, u32, u32, i64, vp, vp]
     L.rmm_debug_sketch_tile.restype = ci
@@ -301,6 +320,205 @@ def rmm_backward(dY, W, X_proj, kind, seed, offset, need_dX=True, need_dbias=Fal
     if rc != 0:
         raise RmmError(rc, "rmm_backward")
     return dX, dW, dbias
+
+
+# ---- 8-bit operands, and the norm in front of them
+
+_F8 = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
+_SCALE = {torch.float32: 0, torch.float8_e8m0fnu: 1}
+
+
+def _blocks8(d):
+    return (d + 127) // 128
+
+
+def _pitch16(d):
+    return (d + 15) // 16 * 16
+
+
+def _check_f8(f8, scale_dtype):
+    if f8 not in _F8:
+        raise TypeError("f8 must be torch.float8_e4m3fn or torch.float8_e5m2")
+    if scale_dtype not in _SCALE:
+        raise TypeError("scale_dtype must be torch.float32 or torch.float8_e8m0fnu")
+
+
+def _new_mat8(rows, cols, weights, f8, scale_dtype, device):
+    """An 8-bit matrix and its scales: rows that start on 16 bytes, scales of rows in rows of a multiple of 16."""
+    data = torch.empty((rows, _pitch16(cols)), dtype=f8, device=device)[:, :cols]
+    if weights:
+        return data, torch.empty((_blocks8(rows), _blocks8(cols)), dtype=scale_dtype, device=device)
+    return data, torch.empty((_blocks8(cols), _pitch16(rows)), dtype=scale_dtype, device=device)[:, :rows]
+
+
+def _mat8(data, scales, name, rows, cols, weights, device):
+    """The descriptor of an 8-bit matrix from its two tensors."""
+    for t, what in ((data, name), (scales, name + "'s scales")):
+        if not t.is_cuda:
+            raise ValueError("%s must be a GPU tensor (the library has no CPU path)" % what)
+        if t.device != device:
+            raise ValueError("%s must be on %s, is on %s" % (what, device, t.device))
+    if data.dtype not in _F8:
+        raise TypeError("%s must be torch.float8_e4m3fn or torch.float8_e5m2" % name)
+    if scales.dtype not in _SCALE:
+        raise TypeError("%s's scales must be torch.float32 or torch.float8_e8m0fnu" % name)
+    want = (_blocks8(rows), _blocks8(cols)) if weights else (_blocks8(cols), rows)
+    if tuple(data.shape) != (rows, cols):
+        raise ValueError("%s must have shape %s, has %s" % (name, (rows, cols), tuple(data.shape)))
+    if tuple(scales.shape) != want:
+        raise ValueError("%s's scales must have shape %s, have %s" % (name, want, tuple(scales.shape)))
+    ld = data.stride(0) if rows > 1 else max(data.stride(0), _pitch16(cols))
+    lds = scales.stride(0) if want[0] > 1 else max(scales.stride(0), want[1] if weights else _pitch16(want[1]))
+    if (cols > 1 and data.stride(1) != 1) or (rows > 1 and (ld % 16 != 0 or ld < cols)):
+        raise ValueError("%s must have contiguous rows that start a multiple of 16 bytes apart (rmm_quantize8 makes such)" % name)
+    if (want[1] > 1 and scales.stride(1) != 1) or (want[0] > 1 and (lds < want[1] or (not weights and lds % 16 != 0))):
+        raise ValueError("%s's scales must have contiguous rows%s" % (name, "" if weights else " that start a multiple of 16 elements apart"))
+    if rows == 1:
+        ld = _pitch16(ld)
+    if want[0] == 1 and not weights:
+        lds = _pitch16(lds)
+    return _Mat8(data.data_ptr(), ld, scales.data_ptr(), lds, _F8[data.dtype], _SCALE[scales.dtype])
+
+
+def _matrix(t, name, dims=2):
+    if not isinstance(t, torch.Tensor) or t.dim() != dims:
+        raise ValueError("%s must be a tensor of %d dimensions" % (name, dims))
+    if t.dtype not in _DTYPES:
+        raise TypeError("%s must be torch.float32 or torch.bfloat16" % name)
+    return t
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError("%s must be on %s, is on %s" % (name, device, t.device))
+
+
+def rmm_quantize8(A, f8=torch.float8_e4m3fn, scale_dtype=torch.float32):
+    """A (n x d) to 8-bit rows with a scale for each 128 columns of a row.  Returns (data, scales): data n x d of dtype `f8`,
+    rows a multiple of 16 bytes apart; scales ceil(d / 128) x n of `scale_dtype` (torch.float32, or torch.float8_e8m0fnu for
+    powers of two), element (b, i) for columns 128 b .. of row i."""
+    r = _native("quantize8", A, f8, scale_dtype)
+    if r is not None:
+        return r
+    _check_f8(f8, scale_dtype)
+    n, d = _matrix(A, "A").shape
+    p = _ptr(A, "A")
+    data, scales = _new_mat8(n, d, False, f8, scale_dtype, A.device)
+    out = _mat8(data, scales, "out", n, d, False, A.device)
+    with torch.cuda.device(A.device):
+        rc = load_library().rmm_quantize8(n, d, _DTYPES[A.dtype], p, ctypes.byref(out), _stream(A))
+    if rc != 0:
+        raise RmmError(rc, "rmm_quantize8")
+    return data, scales
+
+
+def rmm_quantize8_weight(W, f8=torch.float8_e4m3fn, scale_dtype=torch.float32, transposed=False):
+    """W (rows x cols) to 8 bits with a scale for each 128 x 128 block.  Returns (data, scales), scales ceil(rows / 128) x
+    ceil(cols / 128); with `transposed` (data, scales, data_t, scales_t), the same bytes and scales of W^T."""
+    r = _native("quantize8_weight", W, f8, scale_dtype, transposed)
+    if r is not None:
+        return r
+    _check_f8(f8, scale_dtype)
+    rows, cols = _matrix(W, "W").shape
+    p = _ptr(W, "W")
+    data, scales = _new_mat8(rows, cols, True, f8, scale_dtype, W.device)
+    out, out_t, more = _mat8(data, scales, "out", rows, cols, True, W.device), None, ()
+    if transposed:
+        more = _new_mat8(cols, rows, True, f8, scale_dtype, W.device)
+        out_t = ctypes.byref(_mat8(*more, "out_t", cols, rows, True, W.device))
+    with torch.cuda.device(W.device):
+        rc = load_library().rmm_quantize8_weight(rows, cols, _DTYPES[W.dtype], p, ctypes.byref(out), out_t, _stream(W))
+    if rc != 0:
+        raise RmmError(rc, "rmm_quantize8_weight")
+    return (data, scales) + tuple(more)
+
+
+def rmm_linear8(X8, x_scales, W8, w_scales, bias=None, dtype=torch.bfloat16, Y=None):
+    """Y = X W^T (+ bias) of 8-bit operands: X8 (n x d_in, e4m3 or e5m2) with the scales of rows, W8 (d_out x d_in, e4m3) with
+    those of weights, both of one kind.  Returns Y (n x d_out) of `dtype`, summed in fp32.  dX = dY W is the same call on the
+    8-bit rows of dY and the transposed weights of rmm_quantize8_weight."""
+    r = _native("linear8", X8, x_scales, W8, w_scales, bias, dtype, Y)
+    if r is not None:
+        return r
+    if dtype not in _DTYPES:
+        raise TypeError("dtype must be torch.float32 or torch.bfloat16")
+    if X8.dim() != 2 or W8.dim() != 2:
+        raise ValueError("X8 and W8 must be matrices")
+    (n, d_in), d_out = X8.shape, W8.shape[0]
+    x = _mat8(X8, x_scales, "X8", n, d_in, False, X8.device)
+    w = _mat8(W8, w_scales, "W8", d_out, d_in, True, X8.device)
+    if W8.dtype != torch.float8_e4m3fn:
+        raise TypeError("W8 must be torch.float8_e4m3fn")
+    if x_scales.dtype != w_scales.dtype:
+        raise TypeError("X8's and W8's scales must have the same dtype")
+    _same_device(X8.device, bias=bias, Y=Y)
+    bp = _ptr(bias, "bias", dtype, (d_out,), optional=True)
+    if Y is None:
+        Y = torch.empty((n, d_out), dtype=dtype, device=X8.device)
+    yp = _ptr(Y, "Y", dtype, (n, d_out))
+    with torch.cuda.device(X8.device):
+        rc = load_library().rmm_linear8(n, d_in, d_out, _DTYPES[dtype], ctypes.byref(x), ctypes.byref(w), bp, yp, _stream(X8))
+    if rc != 0:
+        raise RmmError(rc, "rmm_linear8")
+    return Y
+
+
+class RMSNormResult(NamedTuple):
+    """What rmm_rms_norm returns; None where it was not asked for."""
+    Y: Optional[torch.Tensor]
+    H: torch.Tensor                 # X + residual, or X itself
+    rstd: torch.Tensor              # n fp32 numbers, for the backward pass
+    Y8: Optional[torch.Tensor]      # Y in 8-bit rows, with their scales as of rmm_quantize8
+    scales: Optional[torch.Tensor]
+
+
+def rmm_rms_norm(X, weight, residual=None, eps=1e-6, need_Y=True, f8=None, scale_dtype=torch.float32):
+    """Root-mean-square norm of the rows of X (n x d), after adding `residual` if there is one.  With `f8` (a float8 dtype) the
+    output comes in 8-bit rows too, made before Y is rounded; need_Y=False leaves Y out."""
+    r = _native("rms_norm", X, weight, residual, eps, need_Y, f8, scale_dtype)
+    if r is not None:
+        return RMSNormResult(*r)
+    n, d = _matrix(X, "X").shape
+    xp, wp = _ptr(X, "X"), _ptr(weight, "weight", X.dtype, (d,))
+    rp = _ptr(residual, "residual", X.dtype, (n, d), optional=True)
+    _same_device(X.device, weight=weight, residual=residual)
+    H = X if residual is None else torch.empty_like(X)
+    Y = torch.empty_like(X) if need_Y else None
+    rstd = torch.empty((n,), dtype=torch.float32, device=X.device)
+    Y8 = scales = out = None
+    if f8 is not None:
+        _check_f8(f8, scale_dtype)
+        Y8, scales = _new_mat8(n, d, False, f8, scale_dtype, X.device)
+        out = ctypes.byref(_mat8(Y8, scales, "Y8", n, d, False, X.device))
+    with torch.cuda.device(X.device):
+        rc = load_library().rmm_rms_norm(n, d, _DTYPES[X.dtype], float(eps), xp, rp, wp, None if residual is None else H.data_ptr(),
+                                         None if Y is None else Y.data_ptr(), out, rstd.data_ptr(), _stream(X))
+    if rc != 0:
+        raise RmmError(rc, "rmm_rms_norm")
+    return RMSNormResult(Y, H, rstd, Y8, scales)
+
+
+def rmm_rms_norm_backward(dY, H, weight, rstd, dH=None, need_dX=True, need_dweight=True):
+    """The norm's backward pass from the forward call's H and rstd.  Returns (dX, dweight); dX is the gradient of X and of the
+    residual.  dH: the gradient that reaches H by other ways."""
+    r = _native("rms_norm_backward", dY, H, weight, rstd, dH, need_dX, need_dweight)
+    if r is not None:
+        return r
+    n, d = _matrix(dY, "dY").shape
+    dp, hp, wp = _ptr(dY, "dY"), _ptr(H, "H", dY.dtype, (n, d)), _ptr(weight, "weight", dY.dtype, (d,))
+    rp, mp = _ptr(rstd, "rstd", torch.float32, (n,)), _ptr(dH, "dH", dY.dtype, (n, d), optional=True)
+    _same_device(dY.device, H=H, weight=weight, rstd=rstd, dH=dH)
+    dX = torch.empty_like(dY) if need_dX else None
+    dweight = torch.empty_like(weight) if need_dweight else None
+    need = int(load_library().rmm_rms_norm_workspace_bytes(n, d, _DTYPES[dY.dtype])) if need_dweight else 0
+    ws, wsp, wsb = _workspace(None, need, dY.device)
+    with torch.cuda.device(dY.device):
+        rc = load_library().rmm_rms_norm_backward(n, d, _DTYPES[dY.dtype], dp, mp, hp, wp, rp, None if dX is None else dX.data_ptr(),
+                                                  None if dweight is None else dweight.data_ptr(), wsp, wsb, _stream(dY))
+    if rc != 0:
+        raise RmmError(rc, "rmm_rms_norm_backward")
+    return dX, dweight
 
 
 def rmm_uses_paired_launch(n, d_in, d_out, k, dtype, kind, op):

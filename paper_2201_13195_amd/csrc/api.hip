@@ -6,20 +6,14 @@
 
 #include <mutex>
 
+#include "api_checks.hpp"
 #include "common.hpp"
 
 using namespace rmm;
 
 namespace {
 
-constexpr int64_t kMaxDim = (int64_t)1 << 31;
-constexpr int64_t kMaxElems = (int64_t)1 << 40;
-
-inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline size_t elem_bytes(int dtype) { return dtype == RMM_DTYPE_BF16 ? 2 : 4; }
-
-bool dims_ok(int64_t a, int64_t b) { return a >= 1 && b >= 1 && a < kMaxDim && b < kMaxDim && a * b < kMaxElems; }
 
 bool desc_ok(const rmm_layer_desc_t *d) {
     if (d == nullptr) return false;
@@ -106,8 +100,6 @@ size_t var_partial_bytes(const rmm_layer_desc_t *d, int64_t room = INT64_MAX) {
 size_t ws_variance(const rmm_layer_desc_t *d, int64_t room = INT64_MAX) {
     return var_partial_bytes(d, room) + (use_mfma(d) ? 0 : round_up((size_t)d->d_in * d->d_out * sizeof(float), 256));
 }
-
-int from_hip(hipError_t e) { return e == hipSuccess ? RMM_OK : RMM_ERR_LAUNCH; }
 
 // Stages that exist only when the two independent products of a pass are launched one by one.
 bool separate_stage(int stage) {
@@ -314,7 +306,7 @@ int backward_impl(const rmm_layer_desc_t *d, SketchState st, const void *dY, con
 
 extern "C" {
 
-int rmm_version(void) { return 400; }
+int rmm_version(void) { return 500; }
 
 const char *rmm_status_string(int status) {
     switch (status) {

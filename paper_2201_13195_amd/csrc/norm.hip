@@ -1,0 +1,396 @@
+// Root-mean-square norm of rows, with the addition of a residual in front and 8-bit rows behind, and its backward pass.
+//
+//   forward    h = x + r (rounded);  rstd = 1 / sqrt(mean h^2 + eps);  y = h rstd w
+//   backward   g = dy w, hhat = h rstd:  dx = rstd (g - hhat mean(g hhat)) + dh;   dw = sum over rows of dy hhat
+//
+// Memory bounds both, so every row is read once and stays in registers until it is written: a lane holds CH runs of
+// eight columns, WPR waves hold a row (8 CH 64 WPR columns), 16 lanes hold a block of 128 columns, whose largest magnitude
+// is then four lane exchanges away.  Work-groups go through the rows in strides, so that the weights are read once a
+// work-group and dw is summed in registers; its partial sums, one row of d numbers a work-group, are added by a second
+// kernel in a fixed order.  Rows too long for the registers of 16 waves are read twice, and their dw has a kernel of its own.
+#include "quant8.hpp"
+
+namespace rmm {
+
+namespace {
+
+constexpr int kRun = 8;  // columns of a lane's run
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+}
+// Sum over the WPR waves of a row, the same in all of them (red: two rows of WPR numbers, taken in turns so that one
+// barrier a row is enough).
+template <int WPR>
+__device__ __forceinline__ float row_sum(float v, float *red, int turn) {
+    v = wave_sum(v);
+    if constexpr (WPR > 1) {
+        float *to = red + (turn & 1) * WPR;
+        if ((threadIdx.x & 63) == 0) to[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < WPR; ++i) v += to[i];
+    }
+    return v;
+}
+
+// Which rows and columns a thread takes.
+template <int WPR>
+struct Place {
+    static constexpr int ROWS = WPR == 1 ? 4 : 1, THREADS = WPR == 16 ? 1024 : 256;
+    int lane, wave, part, row;  // wave of the row, row of the work-group's
+    __device__ __forceinline__ Place()
+        : lane(threadIdx.x & 63), wave(threadIdx.x >> 6), part(WPR == 1 ? 0 : wave), row(WPR == 1 ? wave : 0) {}
+    __device__ __forceinline__ int64_t col(int c) const { return ((int64_t)(c * WPR + part) * 64 + lane) * kRun; }
+};
+
+struct NormArgs {
+    const void *X, *residual, *weight;
+    void *H, *Y;
+    Mat8 y8;
+    int f8, scale;
+    float *rstd;
+    int64_t n, d;
+    float eps;
+};
+
+// Eight columns of y to 8 bits.
+template <int F8, int SCALE>
+__device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col, int lane, const float (&y)[8]) {
+    const BlockScale s = block_scale<F8, SCALE>(max_of_16(amax8(y)));
+    if (col < g.d) {
+        store8_bytes(g.y8.data + row * g.y8.ld + col, g.d - col, to_f8<F8, SCALE>(y, s));
+        if ((lane & 15) == 0) store_scale<SCALE>(g.y8.scales, col / kBlock8 * g.y8.ld_scales + row, s);
+    }
+}
+__device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col, int lane, const float (&y)[8]) {
+    if (g.f8 == F8_E4M3) {
+        if (g.scale == SCALE_F32)
+            put8<F8_E4M3, SCALE_F32>(g, row, col, lane, y);
+        else
+            put8<F8_E4M3, SCALE_E8M0>(g, row, col, lane, y);
+    } else {
+        if (g.scale == SCALE_F32)
+            put8<F8_E5M2, SCALE_F32>(g, row, col, lane, y);
+        else
+            put8<F8_E5M2, SCALE_E8M0>(g, row, col, lane, y);
+    }
+}
+
+// h of eight columns, written to H if there is a residual.
+template <typename T>
+__device__ __forceinline__ void take_h(const NormArgs &g, int64_t row, int64_t col, float (&h)[8]) {
+    const int64_t at = row * g.d + (col < g.d ? col : 0), valid = g.d - col;
+    load8<T>((const T *)g.X + at, valid, h);
+    if (g.residual != nullptr) {
+        float r[8];
+        load8<T>((const T *)g.residual + at, valid, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = rounded<T>(h[i] + r[i]);
+        if (g.H != nullptr) store8<T>((T *)g.H + at, valid, h);
+    }
+}
+
+template <typename T, int CH, int WPR>
+__global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_kernel(NormArgs g) {
+    __shared__ float red[2 * WPR];
+    const Place<WPR> p;
+    float w[CH][8];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) load8<T>((const T *)g.weight + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c), w[c]);
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * p.ROWS + p.row; row < g.n; row += (int64_t)gridDim.x * p.ROWS, ++turn) {
+        float h[CH][8], sum = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) take_h<T>(g, row, p.col(c), h[c]);
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fmaf(h[c][i], h[c][i], sum);
+        const float rstd = 1.0f / sqrtf(row_sum<WPR>(sum, red, turn) / (float)g.d + g.eps);
+        if (g.rstd != nullptr && p.part == 0 && p.lane == 0) g.rstd[row] = rstd;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int64_t col = p.col(c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * rstd * w[c][i];
+            if (g.Y != nullptr) store8<T>((T *)g.Y + row * g.d + (col < g.d ? col : 0), g.d - col, h[c]);
+            if (g.y8.data != nullptr) put8(g, row, col, p.lane, h[c]);
+        }
+    }
+}
+
+// Rows of any length, read twice (the second time mostly from L2).
+template <typename T>
+__global__ void __launch_bounds__(1024) rms_norm_long_kernel(NormArgs g) {
+    __shared__ float red[2 * 16];
+    const Place<16> p;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < g.n; row += gridDim.x, ++turn) {
+        float h[8], sum = 0.0f;
+        for (int c = 0; p.col(c) < g.d; ++c) {
+            take_h<T>(g, row, p.col(c), h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fmaf(h[i], h[i], sum);
+        }
+        const float rstd = 1.0f / sqrtf(row_sum<16>(sum, red, turn) / (float)g.d + g.eps);
+        if (g.rstd != nullptr && threadIdx.x == 0) g.rstd[row] = rstd;
+        NormArgs again = g;  // (what was written is read back, by the thread that wrote it; the buffer may be that of X)
+        if (g.residual != nullptr && g.H != nullptr) again.X = g.H, again.residual = nullptr;
+        again.H = nullptr;
+        for (int c = 0; p.col(c) - p.lane * kRun < g.d; ++c) {  // (whole waves: 16 lanes share a block)
+            const int64_t col = p.col(c);
+            float w[8];
+            take_h<T>(again, row, col, h);
+            load8<T>((const T *)g.weight + (col < g.d ? col : 0), g.d - col, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = h[i] * rstd * w[i];
+            if (g.Y != nullptr) store8<T>((T *)g.Y + row * g.d + (col < g.d ? col : 0), g.d - col, h);
+            if (g.y8.data != nullptr) put8(g, row, col, p.lane, h);
+        }
+    }
+}
+
+struct NormBackwardArgs {
+    const void *dY, *dH, *H, *weight;
+    const float *rstd;
+    void *dX;
+    float *part;  // a row of d numbers for each work-group; null: no dweight
+    int64_t n, d;
+};
+
+template <typename T, int CH, int WPR>
+__global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_backward_kernel(NormBackwardArgs g) {
+    constexpr int PARKED = WPR == 1 ? 3 * CH * 64 * kRun : 1;  // dw of the waves that hold rows of their own
+    __shared__ float red[2 * WPR];
+    __shared__ float parked[PARKED];
+    const Place<WPR> p;
+    const float inv_d = 1.0f / (float)g.d;
+    float w[CH][8], dw[CH][8];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        load8<T>((const T *)g.weight + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c), w[c]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[c][i] = 0.0f;
+    }
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * p.ROWS + p.row; row < g.n; row += (int64_t)gridDim.x * p.ROWS, ++turn) {
+        float dy[CH][8], h[CH][8], sum = 0.0f;
+        const float rstd = g.rstd[row];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int64_t col = p.col(c), at = row * g.d + (col < g.d ? col : 0);
+            load8<T>((const T *)g.dY + at, g.d - col, dy[c]);
+            load8<T>((const T *)g.H + at, g.d - col, h[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                h[c][i] *= rstd;
+                dw[c][i] = fmaf(dy[c][i], h[c][i], dw[c][i]);
+                dy[c][i] *= w[c][i];
+                sum = fmaf(dy[c][i], h[c][i], sum);
+            }
+        if (g.dX == nullptr) continue;  // (the same for all)
+        const float mean = row_sum<WPR>(sum, red, turn) * inv_d;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int64_t col = p.col(c), at = row * g.d + (col < g.d ? col : 0);
+            float more[8];
+            if (g.dH != nullptr) load8<T>((const T *)g.dH + at, g.d - col, more);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float v = rstd * fmaf(-h[c][i], mean, dy[c][i]);
+                dy[c][i] = g.dH != nullptr ? v + more[i] : v;
+            }
+            store8<T>((T *)g.dX + at, g.d - col, dy[c]);
+        }
+    }
+    if (g.part == nullptr) return;
+    if constexpr (WPR == 1) {  // the four waves' sums, in the order of the waves
+        if (p.wave > 0)
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) parked[(((p.wave - 1) * CH + c) * 8 + i) * 64 + p.lane] = dw[c][i];
+        __syncthreads();
+        if (p.wave > 0) return;
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dw[c][i] += parked[((q * CH + c) * 8 + i) * 64 + p.lane];
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int64_t col = p.col(c);
+        store8<float>(g.part + (int64_t)blockIdx.x * g.d + (col < g.d ? col : 0), g.d - col, dw[c]);
+    }
+}
+
+// dX of rows of any length.
+template <typename T>
+__global__ void __launch_bounds__(1024) rms_norm_backward_long_kernel(NormBackwardArgs g) {
+    __shared__ float red[2 * 16];
+    const Place<16> p;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < g.n; row += gridDim.x, ++turn) {
+        const float rstd = g.rstd[row];
+        float dy[8], h[8], w[8], sum = 0.0f;
+        auto take = [&](int64_t col) {
+            const int64_t at = row * g.d + (col < g.d ? col : 0);
+            load8<T>((const T *)g.dY + at, g.d - col, dy);
+            load8<T>((const T *)g.H + at, g.d - col, h);
+            load8<T>((const T *)g.weight + (col < g.d ? col : 0), g.d - col, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] *= rstd, dy[i] *= w[i];
+        };
+        for (int c = 0; p.col(c) < g.d; ++c) {
+            take(p.col(c));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fmaf(dy[i], h[i], sum);
+        }
+        const float mean = row_sum<16>(sum, red, turn) / (float)g.d;
+        for (int c = 0; p.col(c) < g.d; ++c) {
+            const int64_t col = p.col(c), at = row * g.d + col;
+            float more[8];
+            take(col);
+            if (g.dH != nullptr) load8<T>((const T *)g.dH + at, g.d - col, more);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float v = rstd * fmaf(-h[i], mean, dy[i]);
+                dy[i] = g.dH != nullptr ? v + more[i] : v;
+            }
+            store8<T>((T *)g.dX + at, g.d - col, dy);
+        }
+    }
+}
+
+// Partial sums of dw where the rows are too long: work-group (x, y) takes 512 columns, every gridDim.y-th row of four
+// waves.  Runs before dX is written (it may be the buffer of dY).
+template <typename T>
+__global__ void __launch_bounds__(64) rms_norm_dweight_kernel(NormBackwardArgs g) {
+    for (int64_t c0 = (int64_t)blockIdx.x * 512; c0 < g.d; c0 += (int64_t)gridDim.x * 512) {
+        const int64_t col = c0 + threadIdx.x * kRun;
+        float dw[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int64_t row = blockIdx.y; row < g.n; row += gridDim.y) {
+            const int64_t at = row * g.d + (col < g.d ? col : 0);
+            const float rstd = g.rstd[row];
+            float dy[8], h[8];
+            load8<T>((const T *)g.dY + at, g.d - col, dy);
+            load8<T>((const T *)g.H + at, g.d - col, h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dw[i] = fmaf(dy[i], h[i] * rstd, dw[i]);
+        }
+        store8<float>(g.part + (int64_t)blockIdx.y * g.d + (col < g.d ? col : 0), g.d - col, dw);
+    }
+}
+
+// dweight[j] = sum of part[p][j], p = 0 .. parts - 1: 16 columns a work-group, 64 threads a column.
+template <typename T>
+__global__ void __launch_bounds__(1024) sum_parts_kernel(const float *__restrict__ part, int parts, int64_t d, T *__restrict__ out) {
+    __shared__ float sums[64][17];
+    const int c = threadIdx.x & 15, s = threadIdx.x >> 4;
+    for (int64_t c0 = (int64_t)blockIdx.x * 16; c0 < d; c0 += (int64_t)gridDim.x * 16) {
+        float v = 0.0f;
+        if (c0 + c < d)
+#pragma unroll 8
+            for (int p = s; p < parts; p += 64) v += part[(int64_t)p * d + c0 + c];
+        __syncthreads();
+        sums[s][c] = v;
+        __syncthreads();
+        if (threadIdx.x < 64) {  // four threads a column, then their four sums
+            const int cc = threadIdx.x & 15, q = threadIdx.x >> 4;
+            float t = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) t += sums[q * 16 + i][cc];
+            t += __shfl_xor(t, 16, 64);
+            t += __shfl_xor(t, 32, 64);
+            if (q == 0 && c0 + cc < d) store_f32<T>(out + c0 + cc, t);
+        }
+    }
+}
+
+// Columns that CH runs a lane in WPR waves hold.
+constexpr int64_t columns(int ch, int wpr) { return (int64_t)ch * wpr * 64 * kRun; }
+int64_t rows_a_group(int64_t d) { return d <= columns(2, 1) ? 4 : 1; }
+constexpr int64_t kMostForward = 2048, kMostBackward = 512;  // work-groups: eight, two for each compute unit
+bool long_rows(int64_t d) { return d > columns(4, 16); }
+int64_t backward_groups(int64_t n, int64_t d) {
+    if (long_rows(d)) return n < 16 ? n : 16;
+    const int64_t groups = (n + rows_a_group(d) - 1) / rows_a_group(d);
+    return groups < kMostBackward ? groups : kMostBackward;
+}
+
+}  // namespace
+
+size_t norm_backward_partials(int64_t n, int64_t d) { return (size_t)backward_groups(n, d) * (size_t)d; }
+
+template <typename T>
+hipError_t launch_rms_norm(const T *X, const T *residual, const T *weight, T *H, T *Y, const Mat8 *Y8, int f8, int scale, float *rstd,
+                           int64_t n, int64_t d, float eps, hipStream_t stream) {
+    const NormArgs g = {X, residual, weight, H, Y, Y8 != nullptr ? *Y8 : Mat8{nullptr, 0, nullptr, 0}, f8, scale, rstd, n, d, eps};
+    const int64_t groups = (n + rows_a_group(d) - 1) / rows_a_group(d);
+    const unsigned grid = (unsigned)(groups < kMostForward ? groups : kMostForward);
+    if (d <= columns(1, 1))
+        rms_norm_kernel<T, 1, 1><<<grid, 256, 0, stream>>>(g);
+    else if (d <= columns(2, 1))
+        rms_norm_kernel<T, 2, 1><<<grid, 256, 0, stream>>>(g);
+    else if (d <= columns(1, 4))
+        rms_norm_kernel<T, 1, 4><<<grid, 256, 0, stream>>>(g);
+    else if (d <= columns(2, 4))
+        rms_norm_kernel<T, 2, 4><<<grid, 256, 0, stream>>>(g);
+    else if (d <= columns(4, 4))
+        rms_norm_kernel<T, 4, 4><<<grid, 256, 0, stream>>>(g);
+    else if (d <= columns(4, 16))
+        rms_norm_kernel<T, 4, 16><<<grid, 1024, 0, stream>>>(g);
+    else
+        rms_norm_long_kernel<T><<<grid, 1024, 0, stream>>>(g);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_rms_norm_backward(const T *dY, const T *dH, const T *H, const T *weight, const float *rstd, T *dX, T *dweight,
+                                    float *part, int64_t n, int64_t d, hipStream_t stream) {
+    const NormBackwardArgs g = {dY, dH, H, weight, rstd, dX, dweight != nullptr ? part : nullptr, n, d};
+    const unsigned grid = (unsigned)backward_groups(n, d);
+    if (long_rows(d)) {
+        const int64_t wide = (d + 511) / 512;
+        if (dweight != nullptr)
+            rms_norm_dweight_kernel<T><<<dim3((unsigned)(wide < (1 << 20) ? wide : (1 << 20)), grid), 64, 0, stream>>>(g);
+        if (dX != nullptr) rms_norm_backward_long_kernel<T><<<(unsigned)(n < kMostForward ? n : kMostForward), 1024, 0, stream>>>(g);
+    } else if (d <= columns(1, 1)) {
+        rms_norm_backward_kernel<T, 1, 1><<<grid, 256, 0, stream>>>(g);
+    } else if (d <= columns(2, 1)) {
+        rms_norm_backward_kernel<T, 2, 1><<<grid, 256, 0, stream>>>(g);
+    } else if (d <= columns(1, 4)) {
+        rms_norm_backward_kernel<T, 1, 4><<<grid, 256, 0, stream>>>(g);
+    } else if (d <= columns(2, 4)) {
+        rms_norm_backward_kernel<T, 2, 4><<<grid, 256, 0, stream>>>(g);
+    } else if (d <= columns(2, 16)) {
+        rms_norm_backward_kernel<T, 2, 16><<<grid, 1024, 0, stream>>>(g);
+    } else {
+        rms_norm_backward_kernel<T, 4, 16><<<grid, 1024, 0, stream>>>(g);
+    }
+    if (dweight != nullptr) {
+        const int64_t wide = (d + 15) / 16;
+        sum_parts_kernel<T><<<(unsigned)(wide < (1 << 20) ? wide : (1 << 20)), 1024, 0, stream>>>(part, (int)grid, d, dweight);
+    }
+    return hipGetLastError();
+}
+
+#define INSTANCES(T)                                                                                                                 \
+    template hipError_t launch_rms_norm<T>(const T *, const T *, const T *, T *, T *, const Mat8 *, int, int, float *, int64_t, int64_t, \
+                                           float, hipStream_t);                                                                      \
+    template hipError_t launch_rms_norm_backward<T>(const T *, const T *, const T *, const T *, const float *, T *, T *, float *, int64_t, \
+                                                    int64_t, hipStream_t);
+INSTANCES(bf16_t)
+INSTANCES(float)
+#undef INSTANCES
+
+}  // namespace rmm

@@ -1,0 +1,136 @@
+// bf16 / fp32 matrices to 8-bit rows (a scale for each 128 columns of a row) and to 8-bit weights (a scale for each
+// 128 x 128 block, and the transposed matrix from the same read).  Both read every element once and keep it in registers
+// between the maximum and the conversion; memory bounds them.
+#include "quant8.hpp"
+
+namespace rmm {
+
+namespace {
+
+constexpr int kRowsPerGroup = 16;  // rows of a work-group: 16 lanes each
+constexpr int kBlocksPerGroup = 4; // blocks of 128 columns, one after the other, all loaded first
+
+// Work-group (x, y): rows 16 x .., blocks 4 y ..  The 16 lanes of a row read 256 (bf16) or 512 consecutive bytes.
+template <typename T, int F8, int SCALE>
+__global__ void __launch_bounds__(256) quantize_rows8_kernel(const T *__restrict__ A, int64_t n, int64_t d, Mat8 out) {
+    const int lane16 = threadIdx.x & 15;
+    const int64_t row = (int64_t)blockIdx.x * kRowsPerGroup + (threadIdx.x >> 4);
+    if (row >= n) return;  // (16 lanes leave together: those of a row share its maximum)
+    const int64_t blocks = (d + kBlock8 - 1) / kBlock8;
+    for (int64_t b0 = (int64_t)blockIdx.y * kBlocksPerGroup; b0 < blocks; b0 += (int64_t)gridDim.y * kBlocksPerGroup) {
+        float v[kBlocksPerGroup][8];
+#pragma unroll
+        for (int i = 0; i < kBlocksPerGroup; ++i) {
+            const int64_t col = (b0 + i) * kBlock8 + lane16 * 8;
+            load8<T>(A + row * d + (col < d ? col : 0), d - col, v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kBlocksPerGroup; ++i) {
+            if (b0 + i >= blocks) break;
+            const int64_t col = (b0 + i) * kBlock8 + lane16 * 8;
+            const BlockScale s = block_scale<F8, SCALE>(max_of_16(amax8(v[i])));
+            store8_bytes(out.data + row * out.ld + col, d - col, to_f8<F8, SCALE>(v[i], s));
+            if (lane16 == 0) store_scale<SCALE>(out.scales, (b0 + i) * out.ld_scales + row, s);
+        }
+    }
+}
+
+// 4 x 4 bytes: b[j] = byte j of a[0], a[1], a[2], a[3].
+__device__ __forceinline__ void transpose_4x4(uint32_t (&a)[4]) {
+    const uint32_t lo01 = __builtin_amdgcn_perm(a[1], a[0], 0x05010400u), hi01 = __builtin_amdgcn_perm(a[1], a[0], 0x07030602u);
+    const uint32_t lo23 = __builtin_amdgcn_perm(a[3], a[2], 0x05010400u), hi23 = __builtin_amdgcn_perm(a[3], a[2], 0x07030602u);
+    a[0] = __builtin_amdgcn_perm(lo23, lo01, 0x05040100u), a[1] = __builtin_amdgcn_perm(lo23, lo01, 0x07060302u);
+    a[2] = __builtin_amdgcn_perm(hi23, hi01, 0x05040100u), a[3] = __builtin_amdgcn_perm(hi23, hi01, 0x07060302u);
+}
+
+// A work-group for each 128 x 128 block: a thread holds 8 x 8 elements (rows 8 g .., columns 8 l ..), so that it has eight
+// bytes of a row and, transposed in registers, eight of a column to write.
+template <typename T, int F8, int SCALE>
+__global__ void __launch_bounds__(256) quantize_weight8_kernel(const T *__restrict__ W, int64_t rows, int64_t cols, Mat8 out, Mat8 out_t) {
+    __shared__ uint32_t most[4];
+    const int64_t blocks_c = (cols + kBlock8 - 1) / kBlock8, blocks = (rows + kBlock8 - 1) / kBlock8 * blocks_c;
+    for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+        const int64_t br = block / blocks_c, bc = block - br * blocks_c;
+        const int64_t row0 = br * kBlock8 + (threadIdx.x >> 4) * 8, col0 = bc * kBlock8 + (threadIdx.x & 15) * 8;
+        float v[8][8];
+        uint32_t m = 0;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const bool there = row0 + r < rows && col0 < cols;
+            load8<T>(W + (there ? (row0 + r) * cols + col0 : 0), there ? cols - col0 : 0, v[r]);
+        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r) m = max(m, amax8(v[r]));
+        m = max_of_16(m);
+#pragma unroll
+        for (int off = 16; off < 64; off <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off, 64));
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = m;
+        __syncthreads();
+        const BlockScale s = block_scale<F8, SCALE>(max(max(most[0], most[1]), max(most[2], most[3])));
+        uint32_t q[2][8];  // [columns 0-3, 4-7][row]
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const uint2 p = to_f8<F8, SCALE>(v[r], s);
+            q[0][r] = p.x, q[1][r] = p.y;
+            if (row0 + r < rows && col0 < cols) store8_bytes(out.data + (row0 + r) * out.ld + col0, cols - col0, p);
+        }
+        if (threadIdx.x == 0) {
+            store_scale<SCALE>(out.scales, br * out.ld_scales + bc, s);
+            if (out_t.data != nullptr) store_scale<SCALE>(out_t.scales, bc * out_t.ld_scales + br, s);
+        }
+        if (out_t.data != nullptr) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t top[4] = {q[h][0], q[h][1], q[h][2], q[h][3]}, low[4] = {q[h][4], q[h][5], q[h][6], q[h][7]};
+                transpose_4x4(top), transpose_4x4(low);
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (col0 + 4 * h + c < cols && row0 < rows)
+                        store8_bytes(out_t.data + (col0 + 4 * h + c) * out_t.ld + row0, rows - row0, make_uint2(top[c], low[c]));
+            }
+        }
+    }
+}
+
+// The four instances of a kernel template by format and kind of scale.
+#define RMM_BY_FORMAT(CALL)                                                                                             \
+    (f8 == F8_E4M3 ? (scale == SCALE_F32 ? CALL(F8_E4M3, SCALE_F32) : CALL(F8_E4M3, SCALE_E8M0))                        \
+                   : (scale == SCALE_F32 ? CALL(F8_E5M2, SCALE_F32) : CALL(F8_E5M2, SCALE_E8M0)))
+
+}  // namespace
+
+template <typename T>
+hipError_t launch_quantize_rows8(const T *A, int64_t n, int64_t d, int f8, int scale, const Mat8 &out, hipStream_t stream) {
+    const int64_t groups = (n + kRowsPerGroup - 1) / kRowsPerGroup, blocks = (d + kBlock8 - 1) / kBlock8;
+    // (2^31 rows are 2^27 work-groups of 2^8 threads, beyond the 2^32 threads of a launch: those are launched in parts)
+    constexpr int64_t kMost = 1 << 20;
+    for (int64_t g = 0; g < groups; g += kMost) {
+        const int64_t row0 = g * kRowsPerGroup, here = groups - g < kMost ? groups - g : kMost;
+        const int64_t width = (blocks + kBlocksPerGroup - 1) / kBlocksPerGroup, cut = width < 1024 ? width : 1024;
+        const Mat8 o = {out.data + row0 * out.ld, out.ld, (char *)out.scales + row0 * (scale == SCALE_F32 ? 4 : 1), out.ld_scales};
+#define CALL(F, S) (quantize_rows8_kernel<T, F, S><<<dim3((unsigned)here, (unsigned)cut), 256, 0, stream>>>(A + row0 * d, n - row0, d, o), 0)
+        RMM_BY_FORMAT(CALL);
+#undef CALL
+    }
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_quantize_weight8(const T *W, int64_t rows, int64_t cols, int f8, int scale, const Mat8 &out, const Mat8 *out_t,
+                                   hipStream_t stream) {
+    const int64_t blocks = ((rows + kBlock8 - 1) / kBlock8) * ((cols + kBlock8 - 1) / kBlock8);
+    const unsigned grid = (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20));
+    const Mat8 t = out_t != nullptr ? *out_t : Mat8{nullptr, 0, nullptr, 0};
+#define CALL(F, S) (quantize_weight8_kernel<T, F, S><<<grid, 256, 0, stream>>>(W, rows, cols, out, t), 0)
+    RMM_BY_FORMAT(CALL);
+#undef CALL
+    return hipGetLastError();
+}
+
+template hipError_t launch_quantize_rows8<bf16_t>(const bf16_t *, int64_t, int64_t, int, int, const Mat8 &, hipStream_t);
+template hipError_t launch_quantize_rows8<float>(const float *, int64_t, int64_t, int, int, const Mat8 &, hipStream_t);
+template hipError_t launch_quantize_weight8<bf16_t>(const bf16_t *, int64_t, int64_t, int, int, const Mat8 &, const Mat8 *, hipStream_t);
+template hipError_t launch_quantize_weight8<float>(const float *, int64_t, int64_t, int, int, const Mat8 &, const Mat8 *, hipStream_t);
+
+}  // namespace rmm

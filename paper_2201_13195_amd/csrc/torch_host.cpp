@@ -8,6 +8,7 @@
 //   - a negative int: the rmm_status_t of the library call, or
 //   - NotImplemented: something about the arguments is unusual (wrong type, device, shape, layout);
 //     the caller then goes through the checks in binding.py, which say what.
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/function.h>
 #include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_cpp_function.h>
@@ -381,9 +382,179 @@ PyObject *py_infer(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     RMM_END
 }
 
+// ---- 8-bit operands, and the norm in front of them
+
+int f8_code(at::ScalarType t) { return t == at::kFloat8_e4m3fn ? RMM_F8_E4M3 : t == at::kFloat8_e5m2 ? RMM_F8_E5M2 : -1; }
+int scale_code(at::ScalarType t) { return t == at::kFloat ? RMM_SCALE_F32 : t == at::kFloat8_e8m0fnu ? RMM_SCALE_E8M0 : -1; }
+at::ScalarType arg_dtype(PyObject *o) {
+    if (!THPDtype_Check(o)) throw Unusual();
+    return reinterpret_cast<THPDtype *>(o)->scalar_type;
+}
+int64_t blocks8(int64_t d) { return (d + 127) / 128; }
+int64_t pitch16(int64_t d) { return (d + 15) / 16 * 16; }
+
+// rows x cols of a new buffer with rows of `pitch`.
+Tensor new_pitched(const Tensor &like, int64_t rows, int64_t cols, int64_t pitch, at::ScalarType dtype) {
+    Tensor t = at::empty({rows, pitch}, like.options().dtype(dtype).requires_grad(false));
+    if (pitch != cols) t.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef{rows, cols}, at::IntArrayRef{pitch, 1});
+    return t;
+}
+// An 8-bit matrix: its two tensors and the descriptor.
+struct Pair8 {
+    Tensor data, scales;
+    rmm_mat8_t m;
+};
+Pair8 new_mat8(const Tensor &like, int64_t rows, int64_t cols, bool weights, at::ScalarType f8, at::ScalarType scale) {
+    Pair8 p;
+    const int64_t ld = pitch16(cols), lds = weights ? blocks8(cols) : pitch16(rows);
+    p.data = new_pitched(like, rows, cols, ld, f8);
+    p.scales = weights ? new_pitched(like, blocks8(rows), lds, lds, scale) : new_pitched(like, blocks8(cols), rows, lds, scale);
+    p.m = {p.data.data_ptr(), ld, p.scales.data_ptr(), lds, f8_code(f8), scale_code(scale)};
+    return p;
+}
+// The descriptor of given tensors (anything unusual about them is for binding.py to judge).
+rmm_mat8_t old_mat8(const Tensor &data, const Tensor &scales, bool weights, const Tensor &like) {
+    need(data.is_cuda() && scales.is_cuda() && data.device() == like.device() && scales.device() == like.device());
+    need(data.dim() == 2 && scales.dim() == 2 && f8_code(data.scalar_type()) >= 0 && scale_code(scales.scalar_type()) >= 0);
+    const int64_t rows = data.size(0), cols = data.size(1), high = weights ? blocks8(rows) : blocks8(cols), wide = weights ? blocks8(cols) : rows;
+    need(scales.size(0) == high && scales.size(1) == wide);
+    const int64_t ld = rows > 1 ? data.stride(0) : pitch16(std::max(data.stride(0), cols));
+    const int64_t lds = high > 1 ? scales.stride(0) : weights ? std::max(scales.stride(0), wide) : pitch16(std::max(scales.stride(0), wide));
+    need((cols == 1 || data.stride(1) == 1) && ld % 16 == 0 && ld >= cols);
+    need((wide == 1 || scales.stride(1) == 1) && lds >= wide && (weights || lds % 16 == 0));
+    return {data.data_ptr(), ld, scales.data_ptr(), lds, f8_code(data.scalar_type()), scale_code(scales.scalar_type())};
+}
+PyObject *tuple_of(std::initializer_list<Tensor> ts) {
+    PyObject *out = PyTuple_New((Py_ssize_t)ts.size());
+    if (out == nullptr) return nullptr;
+    Py_ssize_t i = 0;
+    for (const Tensor &t : ts) PyTuple_SET_ITEM(out, i++, wrap(t));
+    return out;
+}
+bool is_input(const Tensor &t, int64_t dims) { return t.is_cuda() && t.dim() == dims && t.is_contiguous() && dtype_code(t) >= 0 && t.numel() > 0; }
+
+// quantize8(A, f8, scale_dtype) -> (data, scales)
+PyObject *py_quantize8(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    RMM_BEGIN(3)
+    const Tensor A = arg_tensor(a[0]);
+    const at::ScalarType f8 = arg_dtype(a[1]), scale = arg_dtype(a[2]);
+    need(is_input(A, 2) && f8_code(f8) >= 0 && scale_code(scale) >= 0);
+    const c10::DeviceGuard guard(A.device());
+    const Pair8 out = new_mat8(A, A.size(0), A.size(1), false, f8, scale);
+    void *stream = current_stream(A);
+    int rc;
+    {
+        NoGil free_;
+        rc = rmm_quantize8(A.size(0), A.size(1), dtype_code(A), ptr(A), &out.m, stream);
+    }
+    return rc != RMM_OK ? PyLong_FromLong(rc) : tuple_of({out.data, out.scales});
+    RMM_END
+}
+
+// quantize8_weight(W, f8, scale_dtype, transposed) -> (data, scales[, data_t, scales_t])
+PyObject *py_quantize8_weight(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    RMM_BEGIN(4)
+    const Tensor W = arg_tensor(a[0]);
+    const at::ScalarType f8 = arg_dtype(a[1]), scale = arg_dtype(a[2]);
+    const bool transposed = arg_bool(a[3]);
+    need(is_input(W, 2) && f8_code(f8) >= 0 && scale_code(scale) >= 0);
+    const c10::DeviceGuard guard(W.device());
+    const Pair8 out = new_mat8(W, W.size(0), W.size(1), true, f8, scale);
+    Pair8 t;
+    if (transposed) t = new_mat8(W, W.size(1), W.size(0), true, f8, scale);
+    void *stream = current_stream(W);
+    int rc;
+    {
+        NoGil free_;
+        rc = rmm_quantize8_weight(W.size(0), W.size(1), dtype_code(W), ptr(W), &out.m, transposed ? &t.m : nullptr, stream);
+    }
+    if (rc != RMM_OK) return PyLong_FromLong(rc);
+    return transposed ? tuple_of({out.data, out.scales, t.data, t.scales}) : tuple_of({out.data, out.scales});
+    RMM_END
+}
+
+// linear8(X8, x_scales, W8, w_scales, bias, dtype, Y) -> Y
+PyObject *py_linear8(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    RMM_BEGIN(7)
+    const Tensor X = arg_tensor(a[0]), xs = arg_tensor(a[1]), W = arg_tensor(a[2]), ws = arg_tensor(a[3]), bias = arg_tensor(a[4], true);
+    const at::ScalarType dtype = arg_dtype(a[5]);
+    Tensor Y = arg_tensor(a[6], true);
+    need((dtype == at::kBFloat16 || dtype == at::kFloat) && X.dim() == 2 && W.dim() == 2 && X.size(1) == W.size(1) && X.numel() > 0 && W.numel() > 0);
+    const rmm_mat8_t x = old_mat8(X, xs, false, X), w = old_mat8(W, ws, true, X);
+    need(w.f8 == RMM_F8_E4M3 && w.scale == x.scale);
+    const int64_t n = X.size(0), d_in = X.size(1), d_out = W.size(0);
+    const c10::DeviceGuard guard(X.device());
+    if (!Y.defined()) Y = at::empty({n, d_out}, X.options().dtype(dtype).requires_grad(false));
+    need(Y.scalar_type() == dtype && Y.device() == X.device() && is_matrix(Y, n, d_out, Y));
+    need(!bias.defined() || is_matrix(bias, d_out, -1, Y));
+    void *stream = current_stream(X);
+    int rc;
+    {
+        NoGil free_;
+        rc = rmm_linear8(n, d_in, d_out, dtype == at::kBFloat16 ? RMM_DTYPE_BF16 : RMM_DTYPE_F32, &x, &w, ptr(bias), mut(Y), stream);
+    }
+    return rc != RMM_OK ? PyLong_FromLong(rc) : wrap(Y);
+    RMM_END
+}
+
+// rms_norm(X, weight, residual, eps, need_Y, f8, scale_dtype) -> (Y, H, rstd, Y8, scales)
+PyObject *py_rms_norm(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    RMM_BEGIN(7)
+    const Tensor X = arg_tensor(a[0]), weight = arg_tensor(a[1]), residual = arg_tensor(a[2], true);
+    need(PyFloat_CheckExact(a[3]));
+    const float eps = (float)PyFloat_AS_DOUBLE(a[3]);
+    const bool need_Y = arg_bool(a[4]), eight = a[5] != Py_None;
+    need(is_input(X, 2));
+    const int64_t n = X.size(0), d = X.size(1);
+    need(is_matrix(weight, d, -1, X) && (!residual.defined() || is_matrix(residual, n, d, X)));
+    const c10::DeviceGuard guard(X.device());
+    Pair8 y8;
+    if (eight) {
+        const at::ScalarType f8 = arg_dtype(a[5]), scale = arg_dtype(a[6]);
+        need(f8_code(f8) >= 0 && scale_code(scale) >= 0);
+        y8 = new_mat8(X, n, d, false, f8, scale);
+    }
+    const Tensor H = residual.defined() ? new_matrix(X, n, d) : X, rstd = at::empty({n}, X.options().dtype(at::kFloat).requires_grad(false));
+    const Tensor Y = need_Y ? new_matrix(X, n, d) : Tensor();
+    void *stream = current_stream(X);
+    int rc;
+    {
+        NoGil free_;
+        rc = rmm_rms_norm(n, d, dtype_code(X), eps, ptr(X), ptr(residual), ptr(weight), residual.defined() ? mut(H) : nullptr, mut(Y),
+                                eight ? &y8.m : nullptr, (float *)mut(rstd), stream);
+    }
+    return rc != RMM_OK ? PyLong_FromLong(rc) : tuple_of({Y, H, rstd, y8.data, y8.scales});
+    RMM_END
+}
+
+// rms_norm_backward(dY, H, weight, rstd, dH, need_dX, need_dweight) -> (dX, dweight)
+PyObject *py_rms_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    RMM_BEGIN(7)
+    const Tensor dY = arg_tensor(a[0]), H = arg_tensor(a[1]), weight = arg_tensor(a[2]), rstd = arg_tensor(a[3]), dH = arg_tensor(a[4], true);
+    const bool need_dX = arg_bool(a[5]), need_dw = arg_bool(a[6]);
+    need(is_input(dY, 2));
+    const int64_t n = dY.size(0), d = dY.size(1);
+    need(is_matrix(H, n, d, dY) && is_matrix(weight, d, -1, dY) && (!dH.defined() || is_matrix(dH, n, d, dY)));
+    need(rstd.is_cuda() && rstd.device() == dY.device() && rstd.scalar_type() == at::kFloat && rstd.is_contiguous() && rstd.dim() == 1 &&
+         rstd.size(0) == n);
+    const c10::DeviceGuard guard(dY.device());
+    const Tensor dX = need_dX ? new_matrix(dY, n, d) : Tensor(), dw = need_dw ? at::empty({d}, dY.options().requires_grad(false)) : Tensor();
+    const Tensor ws = need_dw ? scratch(dY, rmm_rms_norm_workspace_bytes(n, d, dtype_code(dY))) : Tensor();
+    void *stream = current_stream(dY);
+    int rc;
+    {
+        NoGil free_;
+        rc = rmm_rms_norm_backward(n, d, dtype_code(dY), ptr(dY), ptr(dH), ptr(H), ptr(weight), (const float *)ptr(rstd), mut(dX), mut(dw),
+                                         mut(ws), need_dw ? ws.nbytes() : 0, stream);
+    }
+    return rc != RMM_OK ? PyLong_FromLong(rc) : tuple_of({dX, dw});
+    RMM_END
+}
+
 #define RMM_METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_##NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RMM_METHOD(forward), RMM_METHOD(backward), RMM_METHOD(sketch), RMM_METHOD(variance_stats),
-                         RMM_METHOD(linear),  RMM_METHOD(infer),    {nullptr, nullptr, 0, nullptr}};
+                         RMM_METHOD(linear),  RMM_METHOD(infer),    RMM_METHOD(quantize8), RMM_METHOD(quantize8_weight),
+                         RMM_METHOD(linear8), RMM_METHOD(rms_norm), RMM_METHOD(rms_norm_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rmm_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 PyTypeObject node_type;

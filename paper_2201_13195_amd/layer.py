@@ -7,6 +7,7 @@ Both run in the native module (binding.host()) where it takes the arguments: its
 costs a fraction of a Python function's.
 """
 import itertools
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -99,3 +100,155 @@ class RMMLinear(torch.nn.Module):
         n = X.numel() // X.shape[-1]
         seed, offset = self.__dict__["last_state"] = self.next_state()
         return RMMLinearFunction.apply(X, self.weight, self.bias, self.sketch_size(n), self.kind, seed, offset)
+
+
+# ---- the layer with its plain products in 8 bits, and the norm in front of it
+
+
+class Rows8(NamedTuple):
+    """Activations in 8-bit rows (binding.rmm_quantize8's data and scales), and the same activations in the layer's dtype where
+    a backward pass will follow (None without gradients: the sketch is all that reads them)."""
+    Y: Optional[torch.Tensor]
+    data: torch.Tensor                # n x d
+    scales: torch.Tensor
+    lead: Tuple[int, ...]             # the leading sizes that the n rows stand for
+
+
+def _rows(X):
+    X = X.reshape(-1, X.shape[-1])
+    return X if X.is_contiguous() else X.contiguous()
+
+
+class RMMNormFunction(torch.autograd.Function):
+    """(Y, H, Y8, scales) of binding.rmm_rms_norm; gradients of X, residual and weight from those of Y and H."""
+
+    @staticmethod
+    def forward(ctx, X, residual, weight, eps, f8, scale_dtype, need_Y):
+        r = binding.rmm_rms_norm(_rows(X), weight.contiguous(), None if residual is None else _rows(residual), eps, need_Y, f8, scale_dtype)
+        ctx.set_materialize_grads(False)
+        H = X if residual is None else r.H.reshape(X.shape)
+        ctx.save_for_backward(H, weight, r.rstd)
+        ctx.has_residual = residual is not None
+        if r.Y8 is not None:
+            ctx.mark_non_differentiable(r.Y8, r.scales)
+        return None if r.Y is None else r.Y.reshape(X.shape), None if residual is None else H, r.Y8, r.scales
+
+    @staticmethod
+    def backward(ctx, dY, dH, _, __):
+        H, weight, rstd = ctx.saved_tensors
+        dX, dweight = dH, None
+        if dY is not None:
+            need_dX, need_dw = ctx.needs_input_grad[0] or ctx.needs_input_grad[1], ctx.needs_input_grad[2]
+            if need_dX or need_dw:
+                dX, dweight = binding.rmm_rms_norm_backward(_rows(dY), _rows(H), weight.contiguous(), rstd, None if dH is None else _rows(dH),
+                                                            need_dX, need_dw)
+            dX = None if dX is None else dX.reshape(H.shape)
+        return dX, dX if ctx.has_residual else None, dweight, None, None, None, None
+
+
+class RMMNorm(torch.nn.Module):
+    """Root-mean-square norm over the last dimension: Y = H / sqrt(mean H^2 + eps) * weight, H = X (+ residual).
+    `norm(X)` returns Y, `norm(X, residual)` returns (Y, H).  With `f8` (a float8 dtype) Y comes as Rows8, which RMMLinear8 takes
+    as it is: the 8-bit rows cost no pass of their own."""
+
+    def __init__(self, features, eps=1e-6, f8=None, scale_dtype=torch.float32, device="cuda", dtype=torch.bfloat16):
+        super().__init__()
+        self.eps, self.f8, self.scale_dtype = float(eps), f8, scale_dtype
+        self.weight = torch.nn.Parameter(torch.ones((features,), device=device, dtype=dtype))
+
+    def forward(self, X, residual=None):
+        if residual is not None and residual.shape != X.shape:
+            raise ValueError("residual must have the shape of X, %s, has %s" % (tuple(X.shape), tuple(residual.shape)))
+        need_Y = self.f8 is None or torch.is_grad_enabled()
+        Y, H, Y8, scales = RMMNormFunction.apply(X, residual, self.weight, self.eps, self.f8, self.scale_dtype, need_Y)
+        if self.f8 is not None:
+            Y = Rows8(Y, Y8, scales, tuple(X.shape[:-1]))
+        return Y if residual is None else (Y, H)
+
+
+class RMMLinear8Function(torch.autograd.Function):
+    """Y = X8 W8^T (+ b); backward: dX = dY8 W8, dW = (S^T dY)^T (S^T X) from X and dY before they are rounded, db = dY^T 1.
+    The roundings to 8 bits have derivative one.  Kept for the backward pass: W and X_proj, as in RMMLinearFunction; the 8-bit
+    weights are made again there (they would be as much memory as the saved activations)."""
+
+    @staticmethod
+    def forward(ctx, X, data, scales, W, bias, k, kind, seed, offset, scale_dtype, grad_f8):
+        X2, Wc = _rows(X), W.contiguous()
+        if data is None:
+            data, scales = binding.rmm_quantize8(X2, scale_dtype=scale_dtype)
+        w8, w_scales = binding.rmm_quantize8_weight(Wc, scale_dtype=scale_dtype)
+        Y = binding.rmm_linear8(data, scales, w8, w_scales, bias, X.dtype)
+        X_proj = binding.rmm_sketch(X2, k, kind, seed, offset)
+        ctx.save_for_backward(Wc, X_proj)
+        ctx.state, ctx.formats = (kind, seed, offset), (scale_dtype, grad_f8)
+        ctx.lead, ctx.has_bias = X.shape[:-1], bias is not None
+        return Y.reshape(*X.shape[:-1], W.shape[0])
+
+    @staticmethod
+    def backward(ctx, dY):
+        W, X_proj = ctx.saved_tensors
+        scale_dtype, grad_f8 = ctx.formats
+        dY2, dX, dW, db = _rows(dY), None, None, None
+        if ctx.needs_input_grad[0]:
+            w8 = binding.rmm_quantize8_weight(W, scale_dtype=scale_dtype, transposed=True)
+            dX = binding.rmm_linear8(*binding.rmm_quantize8(dY2, f8=grad_f8, scale_dtype=scale_dtype), *w8[2:], None, dY.dtype)
+            dX = dX.reshape(*ctx.lead, W.shape[1])
+        need_db = ctx.has_bias and ctx.needs_input_grad[4]
+        if ctx.needs_input_grad[3] or need_db:
+            _, dW, db = binding.rmm_backward(dY2, W, X_proj, *ctx.state, need_dX=False, need_dbias=need_db)
+        return (dX, None, None, dW if ctx.needs_input_grad[3] else None, db) + (None,) * 6
+
+
+class RMMLinear8(RMMLinear):
+    """RMMLinear with Y and dX as products of 8-bit operands: X, dY in rows with a scale for each 128 columns, W with one for each
+    128 x 128 block, made anew from W in every call; the weight gradient is RMMLinear's sketched estimate.  Takes a tensor, or the
+    Rows8 of an RMMNorm in front of it.  `scale_dtype`: torch.float32, or torch.float8_e8m0fnu for powers of two;
+    `grad_f8`: the format of dY's rows.
+
+    pack() keeps W's 8-bit form for calls without gradients, until W changes."""
+
+    def __init__(self, in_features, out_features, bias=True, rho=0.1, k=None, kind=binding.GAUSSIAN, seed=0, layer_id=None,
+                 device="cuda", dtype=torch.bfloat16, scale_dtype=torch.float8_e8m0fnu, grad_f8=torch.float8_e4m3fn):
+        super().__init__(in_features, out_features, bias, rho, k, kind, seed, layer_id, device, dtype)
+        binding._check_f8(grad_f8, scale_dtype)
+        self.scale_dtype, self.grad_f8, self._packed = scale_dtype, grad_f8, None
+
+    def _apply(self, fn, recurse=True):
+        self._packed = None
+        return super()._apply(fn, recurse)
+
+    def pack(self):
+        W = self.weight.detach()
+        self._packed = (binding.rmm_quantize8_weight(W.contiguous(), scale_dtype=self.scale_dtype), self.weight, self.weight._version)
+        return self
+
+    def _weight8(self):
+        if self._packed is None:
+            return binding.rmm_quantize8_weight(self.weight.detach().contiguous(), scale_dtype=self.scale_dtype)
+        w8, of, version = self._packed
+        if of is not self.weight or version != self.weight._version:
+            raise RuntimeError("RMMLinear8: the weight has changed since pack(); call pack() again")
+        return w8
+
+    def forward(self, X):
+        rows = X if isinstance(X, Rows8) else None
+        if rows is not None and rows.data.shape[1] != self.in_features:
+            raise ValueError("RMMLinear8: rows of %d columns, in_features is %d" % (rows.data.shape[1], self.in_features))
+        if not torch.is_grad_enabled():
+            if rows is None:
+                lead = X.shape[:-1]
+                data, scales = binding.rmm_quantize8(_rows(X), scale_dtype=self.scale_dtype)
+            else:
+                data, scales, lead = rows.data, rows.scales, rows.lead
+            bias = None if self.bias is None else self.bias.detach()
+            return binding.rmm_linear8(data, scales, *self._weight8(), bias, self.weight.dtype).reshape(*lead, self.out_features)
+        if rows is not None:
+            if rows.Y is None:
+                raise ValueError("RMMLinear8: these rows were made without gradients; a backward pass needs them in the layer's dtype too")
+            X, data, scales = rows.Y, rows.data, rows.scales
+        else:
+            data = scales = None
+        n = X.numel() // X.shape[-1]
+        seed, offset = self.__dict__["last_state"] = self.next_state()
+        return RMMLinear8Function.apply(X, data, scales, self.weight, self.bias, self.sketch_size(n), self.kind, seed, offset,
+                                        self.scale_dtype, self.grad_f8)
