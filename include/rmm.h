@@ -274,7 +274,7 @@ typedef enum { RMM_SCALE_F32 = 0, RMM_SCALE_E8M0 = 1 } rmm_scale_t;
 /* An 8-bit matrix on the device; the call says how many rows and columns it has and which of the two
  * layouts its scales have.  data: rows of `ld` bytes, ld at least the columns and a multiple of 16,
  * 16-byte aligned; what lies behind a row's columns is neither read as a number nor written.  scales:
- * 16-byte aligned, of rows also ld_scales a multiple of 16 elements. */
+ * 16-byte aligned, of rows also ld_scales a multiple of 16 elements; of weights at most 2^26. */
 typedef struct {
     void *data;
     int64_t ld;

@@ -15,7 +15,7 @@ bool mat8_ok(const rmm_mat8_t *m, int64_t rows, int64_t cols, bool weights) {
     if (m->scale != RMM_SCALE_F32 && m->scale != RMM_SCALE_E8M0) return false;
     if (m->ld < cols || m->ld % 16 != 0 || m->ld > kMaxDim || rows * m->ld >= 2 * kMaxElems) return false;
     const int64_t blocks = (cols + kBlock8 - 1) / kBlock8;
-    if (weights) return m->ld_scales >= blocks && m->ld_scales <= kMaxDim;
+    if (weights) return m->ld_scales >= blocks && m->ld_scales <= ((int64_t)1 << 26);
     return m->ld_scales >= rows && m->ld_scales % 16 == 0 && m->ld_scales <= kMaxDim;
 }
 Mat8 as_mat8(const rmm_mat8_t *m) { return Mat8{(uint8_t *)m->data, m->ld, m->scales, m->ld_scales}; }

@@ -1,0 +1,6 @@
+// Tiles of 8-bit products: X in e4m3, scales in fp32, Y in fp32.
+#include "linear8_tile.hpp"
+
+namespace rmm {
+template void launch_linear8_tiles<F8_E4M3, SCALE_F32, float>(const Linear8Args &, bool, hipStream_t);
+}  // namespace rmm

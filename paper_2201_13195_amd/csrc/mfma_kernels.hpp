@@ -26,6 +26,7 @@
 #include <type_traits>
 
 #include "colsum.hpp"
+#include "lds_loads.hpp"
 #include "mfma_frag.hpp"
 #include "row_norms.hpp"
 #include "tile_range.hpp"
@@ -277,32 +278,12 @@ __device__ __forceinline__ void write_tile(const GemmArgs &g, const f32x16_t (&a
 // LDS is laid out by the load, so what keeps bank conflicts away is which chunk a lane asks for: rows of 64 contraction
 // elements hold chunk c at kchunk_pos, rows of columns at col_chunk.
 
-// One wave's load of 1 KB into LDS from byte `to` on, 16 bytes from `off` + `soff` per lane.  The compiler does
-// not see that it writes LDS (it would wait for it before every LDS read): the explicit waits and barriers order them.
-__device__ __forceinline__ void load_to_lds(u32x4_t rsrc, uint32_t to, uint32_t off, uint32_t soff) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(rsrc), "s"(soff) : "m0");
-}
-// The same from `off`.
-__device__ __forceinline__ void load_to_lds(u32x4_t rsrc, uint32_t to, uint32_t off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(rsrc) : "m0");
-}
-// Waits until at most N of this wave's loads are outstanding.
-template <int N>
-__device__ __forceinline__ void wait_for_loads() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
 // A descriptor of `rows` rows of pitch ld from `base` on.  (The same in every lane; saying so keeps it in scalar registers.)
 __device__ __forceinline__ u32x4_t rows_descriptor(const bf16_t *base, int64_t ld, int64_t rows) {
     const uint64_t at = reinterpret_cast<uint64_t>(base);
     return (u32x4_t){(uint32_t)__builtin_amdgcn_readfirstlane((int)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)),
                      (uint32_t)__builtin_amdgcn_readfirstlane((int)((rows > 0 ? rows : 0) * ld * 2)), 0x00020000u};
 }
-// The wait states between a vector instruction that writes a scalar register (a readfirstlane, a spilled one that comes back) and a
-// load that reads it: the compiler does not look for them in front of load_to_lds.  What a step of a K-contiguous operand writes (the range
-// of its descriptor, the offset along its rows) is scalar instructions, which need none, and is not settled: twenty clocks a step and
-// operand, 64 x 64 tiles of Y 5 % (1024 x 1024 -> 512 5.8 and 6.1 us).  That the compiler brings none of it back from a vector register too
-// close to a load is looked for in the built library (tests/test_load_hazards.py).
-__device__ __forceinline__ void settle(u32x4_t &descriptor) { asm volatile("s_nop 4" : "+s"(descriptor)); }
 // The steps of 64 contraction elements in the order in which a work-group takes them: from `start` on and around.  What a request
 // needs is prepared one step ahead, between MFMAs, from what the one before it needed, in scalar registers and mostly 32 bits.  Made
 // anew, with products of 64 bits, selects and a way through the vector unit, it was 45 of the 62 scalar instructions of a step of
