@@ -1,0 +1,6 @@
+// Products of 8-bit operands: X in e5m2, scales in fp32, Y in fp32.
+#include "linear8_launch.hpp"
+
+namespace rmm {
+template void launch_linear8_by<F8_E5M2, SCALE_F32, float>(int, const Linear8Args &, hipStream_t);
+}  // namespace rmm

@@ -17,9 +17,9 @@ struct Linear8Args {
     int64_t n, d_in, d_out;
 };
 
-// The product on tiles (linear8_tiles_*.hip, an instance each).
+// The product by the kernel that linear8_plan() names (linear8_<X>_<scales>_<Y>.hip, an instance each).
 template <int F8, int SCALE, typename T>
-void launch_linear8_tiles(const Linear8Args &g, bool large, hipStream_t stream);
+void launch_linear8_by(int kernel, const Linear8Args &g, hipStream_t stream);
 
 namespace {
 
@@ -83,52 +83,40 @@ __device__ __forceinline__ f32x4_t block_products(const bf16x8_t (&w)[4], const 
 // because the compiler never gives the scaled instruction the same registers for the sum that goes in and the one that comes out: twice
 // the accumulators, and copies.  (The two wait states are for an operand that a vector instruction has just written, which the
 // compiler does not look for in front of assembly; results are read behind settle_sums.)
-template <int F8, int J, bool ACC_VGPR>
+template <int F8, int J>
 __device__ __forceinline__ void add_scaled_products(const i32x8_t &w, const i32x8_t &x, f32x4_t &acc, uint32_t ws, uint32_t xs) {
-#define RMM_SCALED(REG, SEL)                                                                                                       \
+#define RMM_SCALED(SEL)                                                                                                            \
     if constexpr (F8 == F8_E4M3)                                                                                                   \
         asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 " SEL                                  \
-                     : "+" REG(acc)                                                                                                \
+                     : "+v"(acc)                                                                                                   \
                      : "v"(w), "v"(x), "v"(ws), "v"(xs)                                                                            \
                      : "memory");                                                                                                  \
     else                                                                                                                           \
         asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 " SEL " blgp:1"                        \
-                     : "+" REG(acc)                                                                                                \
+                     : "+v"(acc)                                                                                                   \
                      : "v"(w), "v"(x), "v"(ws), "v"(xs)                                                                            \
                      : "memory");
-#define RMM_BY_BYTE(REG)                                              \
-    if constexpr (J == 0) {                                           \
-        RMM_SCALED(REG, "op_sel_hi:[0,0,0]")                          \
-    } else if constexpr (J == 1) {                                    \
-        RMM_SCALED(REG, "op_sel:[0,1,0] op_sel_hi:[0,0,0]")           \
-    } else if constexpr (J == 2) {                                    \
-        RMM_SCALED(REG, "op_sel_hi:[0,1,0]")                          \
-    } else {                                                          \
-        RMM_SCALED(REG, "op_sel:[0,1,0] op_sel_hi:[0,1,0]")           \
-    }
-    if constexpr (ACC_VGPR) {
-        RMM_BY_BYTE("v")
+    if constexpr (J == 0) {
+        RMM_SCALED("op_sel_hi:[0,0,0]")
+    } else if constexpr (J == 1) {
+        RMM_SCALED("op_sel:[0,1,0] op_sel_hi:[0,0,0]")
+    } else if constexpr (J == 2) {
+        RMM_SCALED("op_sel_hi:[0,1,0]")
     } else {
-        RMM_BY_BYTE("a")
+        RMM_SCALED("op_sel:[0,1,0] op_sel_hi:[0,1,0]")
     }
-#undef RMM_BY_BYTE
 #undef RMM_SCALED
 }
 // Keeps the making of a value, and the memory accesses around it, in their places.
 __device__ __forceinline__ void pin(f32x4_t &v) { asm volatile("" : "+v"(v) : : "memory"); }
 // Between the last of these and the first use of their sums (19 wait states would do for the longest of matrix instructions).
-template <bool ACC_VGPR, int TU, int TJ>
+template <int TU, int TJ>
 __device__ __forceinline__ void settle_sums(f32x4_t (&acc)[TU][TJ]) {
     asm volatile("s_nop 15\n\ts_nop 15");
 #pragma unroll
     for (int u = 0; u < TU; ++u)
 #pragma unroll
-        for (int j = 0; j < TJ; ++j) {
-            if constexpr (ACC_VGPR)
-                asm volatile("" : "+v"(acc[u][j]));
-            else
-                asm volatile("" : "+a"(acc[u][j]));
-        }
+        for (int j = 0; j < TJ; ++j) asm volatile("" : "+v"(acc[u][j]));
 }
 
 // Four consecutive outputs o .. o + 3 of a row, of which `valid` exist.

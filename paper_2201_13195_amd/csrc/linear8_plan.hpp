@@ -1,0 +1,50 @@
+// Which kernel a product of 8-bit operands takes (plain C++).
+#pragma once
+#include <stdint.h>
+
+namespace rmm {
+
+// Tokens x outputs of a work-group.  FEW: eight waves share the contraction (linear8_few.hpp); MANY: four, where there are
+// more work-groups than compute units; TILE: linear8_tile.hpp.
+enum {
+    LINEAR8_FEW_16x16 = 0,
+    LINEAR8_FEW_16x32 = 1,
+    LINEAR8_FEW_32x32 = 2,
+    LINEAR8_FEW_64x32 = 3,
+    LINEAR8_MANY_16x64 = 4,
+    LINEAR8_MANY_32x32 = 5,
+    LINEAR8_TILE_128 = 6,
+    LINEAR8_TILE_256 = 7
+};
+
+// A row per rule, times in us of bf16 results measured on both sides of it (256 compute units):
+//   - the smallest FEW kernel with no more work-groups than compute units: its time is one round of a latency and the contraction.
+//       24 x 4096 -> 1024 16x16 6.2, 16x32 7.9, 128 x 128 tiles 20;   128 x 768 -> 768 16x16 4.0 (384 work-groups), 16x32 3.6, 32x32 4.2;
+//       64 x 4096 -> 4096 16x32 13.7 (512), 32x32 10.5, 64x32 14.8;   333 x 1000 -> 1111 32x32 7.0 (385), 64x32 5.7, 128 x 128 tiles 10.5
+//   - up to 32 tokens and more outputs than that: the weights are read once, whatever the tile, and four waves of more outputs keep more of
+//     them in flight.  1 x 4096 -> 32000 (131 MB) 16x16 32.9, MANY 16x64 21.9, 128 x 128 tiles 27.5;  32 x 4096 -> 16384 MANY 32x32 18.6,
+//     128 x 128 tiles 26.4.  33 tokens and more would read them twice: 33 x 1024 -> 16384 MANY 32x32 9.7, 128 x 128 tiles 8.3
+//   - tiles otherwise.  A 256 x 256 tile is 1.2 us a step of 128 and 3 us of its own, with a compute unit to itself; two 128 x 128 tiles
+//     share one, 0.95 us a step of both and 2 us:  8192 x 1024 -> 1024 256 18.8, 128 14.5;  4096 x 1024 -> 4096 256 21.8, 128 24.5;
+//     16384 x 4096 -> 4096 256 207, 128 255.  fp32 results have 128 x 128 tiles alone (the exact way needs the registers).
+inline int64_t linear8_groups(int64_t n, int64_t d_out, int64_t tokens, int64_t outputs) {
+    return ((n + tokens - 1) / tokens) * ((d_out + outputs - 1) / outputs);
+}
+inline int linear8_plan(int64_t n, int64_t d_in, int64_t d_out, int64_t ld_x, int64_t ld_w, bool exact) {
+    constexpr int64_t kUnits = 256;
+    if (linear8_groups(n, d_out, 16, 16) <= kUnits) return LINEAR8_FEW_16x16;
+    if (linear8_groups(n, d_out, 16, 32) <= kUnits) return LINEAR8_FEW_16x32;
+    if (linear8_groups(n, d_out, 32, 32) <= kUnits) return LINEAR8_FEW_32x32;
+    if (linear8_groups(n, d_out, 64, 32) <= kUnits) return LINEAR8_FEW_64x32;
+    if (n <= 16) return LINEAR8_MANY_16x64;
+    const int64_t small = linear8_groups(n, d_out, 128, 128), large = linear8_groups(n, d_out, 256, 256);
+    const bool fits = ld_x < (1 << 23) && ld_w < (1 << 23) && small < (1 << 23);  // (offsets within a tile, and the grid, in 32 bits)
+    if (n <= 32 || !fits) return LINEAR8_MANY_32x32;
+    if (exact) return LINEAR8_TILE_128;
+    const int64_t steps = (d_in + 127) / 128;
+    const int64_t t256 = 600 + (large + kUnits - 1) / kUnits * (120 * steps + 300);
+    const int64_t t128 = 300 + (small + 2 * kUnits - 1) / (2 * kUnits) * (95 * steps + 200);
+    return t256 <= t128 ? LINEAR8_TILE_256 : LINEAR8_TILE_128;
+}
+
+}  // namespace rmm

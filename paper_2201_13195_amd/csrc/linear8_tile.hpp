@@ -32,46 +32,56 @@ __device__ __forceinline__ void for_each(F f) {
     for_each_of(std::make_integer_sequence<int, N>(), f);
 }
 
-// BT x BO outputs on NT x NO waves; PD fragments of W are read ahead, so that one barrier a step stands PD fragments before its
-// end; the loads of a step are spread over SPAN MFMAs behind it.
-template <int BT_, int BO_, int NT_, int NO_, int PD_, int SPAN_, int PER_SIMD_>
+// BT x BO outputs on NT x NO waves, STAGES steps of operands in LDS or on their way; PD fragments of W are read ahead, so that one
+// barrier a step stands PD fragments before its end; the loads of a step are spread over SPAN MFMAs behind it.
+template <int BT_, int BO_, int NT_, int NO_, int STAGES_, int SPAN_, int PER_SIMD_>
 struct Tile8 {
-    static constexpr int BT = BT_, BO = BO_, NT = NT_, NO = NO_, PD = PD_, SPAN = SPAN_, PER_SIMD = PER_SIMD_;
+    static constexpr int BT = BT_, BO = BO_, NT = NT_, NO = NO_, STAGES = STAGES_, PD = 3, SPAN = SPAN_, PER_SIMD = PER_SIMD_;
     static constexpr int WAVES = NT * NO, THREADS = 64 * WAVES;
     static constexpr int WT = BT / NT, WO = BO / NO, TJ = WT / 16, TU = WO / 16;  // of a wave: rows, 16-row tiles
     static constexpr int JX = BT / 8 / WAVES, JW = BO / 8 / WAVES, LOADS = JX + JW + 1;  // 1 KB loads of a wave and step, one of scales
     static constexpr int X_BYTES = BT * 128, W_BYTES = BO * 128, STAGE = X_BYTES + W_BYTES;
     static constexpr int XS_BYTES = BT * 4, SCALES = XS_BYTES + 256;  // of a stage: X's, W's
-    static constexpr int LDS_BYTES = 2 * STAGE + 2 * SCALES + 256;  // (the last 256: of waves without a share of the scales)
+    static constexpr int LDS_BYTES = STAGES * (STAGE + SCALES) + 256;  // (the last 256: of waves without a share of the scales)
     static constexpr int MFMAS = TU * TJ;
     static_assert(BT % (8 * WAVES) == 0 && BO % (8 * WAVES) == 0 && WT % 64 == 0 && WO % 64 == 0 && 128 % WO == 0, "shares of a wave");
-    static_assert(PD == 3 && TU % 4 == 0 && SPAN <= MFMAS && LDS_BYTES <= 160 * 1024, "ring of four fragments");
+    static_assert(PD == 3 && TU % 4 == 0 && SPAN <= PD * TJ && STAGES >= 2 && LDS_BYTES <= 160 * 1024, "ring of four fragments, loads behind the barrier");
 };
 
-// One row-major operand on its way into LDS, J loads of a wave: 32-bit offsets from the tile's first row.
+// A wave-uniform value, which the compiler then keeps in a scalar register.
+__device__ __forceinline__ uint32_t scalar(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ uint64_t scalar(uint64_t v) { return scalar((uint32_t)v) | (uint64_t)scalar((uint32_t)(v >> 32)) << 32; }
+
+// Bytes that a descriptor spans: the rows of an operand that a tile has, dense up to their pitch.
+struct Span {
+    uint64_t base;
+    uint32_t range;
+    __device__ __forceinline__ u32x4_t descriptor() const { return (u32x4_t){(uint32_t)base, (uint32_t)(base >> 32), range, 0x00020000u}; }
+};
+__device__ __forceinline__ Span rows_of(const Mat8 &m, int64_t row0, int64_t rows, bool there) {
+    return {scalar(reinterpret_cast<uint64_t>(m.data) + (uint64_t)(row0 * m.ld)), scalar(there ? (uint32_t)(rows * m.ld) : 0u)};
+}
+
+// One row-major operand on its way into LDS, J loads of a wave: 32-bit offsets from the tile's first row.  Rows that the tile does
+// not have lie behind the descriptor's range: zeros.
 template <int J>
 struct Loads8 {
-    u32x4_t rsrc;
-    uint32_t off[J], beyond[2], to, range;
+    Span at;
+    uint32_t off[J], beyond[2], to;
     // `row_of`: which row (of the tile) LDS row r holds
     template <typename F>
-    __device__ __forceinline__ void init(const uint8_t *first, int64_t ld, int64_t rows, int64_t d, uint32_t lds, int wave, int lane, F row_of) {
-        const uint64_t at = reinterpret_cast<uint64_t>(first);
-        range = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(rows * ld));
-        rsrc = (u32x4_t){(uint32_t)__builtin_amdgcn_readfirstlane((int)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)), range, 0x00020000u};
+    __device__ __forceinline__ void init(int64_t ld, int64_t d, uint32_t lds, int wave, int lane, F row_of) {
         to = lds + (uint32_t)(wave * J * 1024);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int row = (wave * J + j) * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
-            const int64_t from = row_of(row);
-            off[j] = from < rows ? (uint32_t)(from * ld) + (uint32_t)chunk * 16u : 0x80000000u;
+            off[j] = (uint32_t)row_of(row) * (uint32_t)ld + (uint32_t)chunk * 16u;
             if (j < 2) beyond[j] = chunk * 16 < (int)((d - 1) % 128) + 1 ? 0u : 0x80000000u;  // in the last step
         }
-        settle(rsrc);
     }
     // Load j of the step at byte `soff` of the rows into stage byte `stage`.
     __device__ __forceinline__ void load(int j, uint32_t stage, uint32_t soff, uint32_t last) const {
-        load_to_lds(rsrc, to + stage + (uint32_t)j * 1024u, off[j] | (last & beyond[j & 1]), soff);
+        load_to_lds(at.descriptor(), to + stage + (uint32_t)j * 1024u, off[j] | (last & beyond[j & 1]), soff);
     }
 };
 
@@ -86,33 +96,36 @@ template <typename S, int SCALE>
 struct ScaleLoads8 {
     static constexpr int SIZE = SCALE == SCALE_F32 ? 4 : 1, XL = S::BT * SIZE <= 256 ? 1 : S::BT * SIZE / 256;
     static_assert(XL + 1 <= S::WAVES, "a wave loads at most one share of the scales");
-    uint64_t base, base_step;  // X: from step to step
-    uint32_t off, off_step, range, to, stage_bytes;
-    __device__ __forceinline__ void init(const Linear8Args &g, int64_t t0, int64_t o0, uint32_t lds, uint32_t idle, int wave, int lane) {
+    Span at, next;               // (the next tile's)
+    uint64_t base_step;          // X: from step to step
+    uint32_t off, next_off, off_step, to, stage_bytes;
+    __device__ __forceinline__ void init(const Linear8Args &g, uint32_t lds, uint32_t idle, int wave) {
+        base_step = scalar(wave < XL ? (uint64_t)g.x.ld_scales * SIZE : (uint64_t)0), off_step = scalar(wave == XL ? (uint32_t)SIZE : 0u);
+        to = scalar(wave < XL ? lds + (uint32_t)wave * 256u : wave == XL ? lds + (uint32_t)S::XS_BYTES : idle), stage_bytes = scalar(wave <= XL ? (uint32_t)S::SCALES : 0u);
+    }
+    // Where the scales of a tile begin.
+    __device__ __forceinline__ void place(const Linear8Args &g, int64_t t0, int64_t o0, bool there, int wave, int lane) {
+        uint64_t base = reinterpret_cast<uint64_t>(g.x.scales);
+        uint32_t range = 0;
+        next_off = 0x80000000u;
         if (wave < XL) {
             const int64_t first = t0 + wave * (256 / SIZE), left = g.n - first;
-            base = reinterpret_cast<uint64_t>(g.x.scales) + (uint64_t)first * SIZE, base_step = (uint64_t)g.x.ld_scales * SIZE;
-            range = left > 0 ? (uint32_t)((min((int64_t)(256 / SIZE), left) * SIZE + 3) & ~(int64_t)3) : 0u;
-            off = lane * 4, off_step = 0, to = lds + wave * 256, stage_bytes = S::SCALES;
+            base += (uint64_t)first * SIZE, range = left > 0 ? (uint32_t)((min((int64_t)(256 / SIZE), left) * SIZE + 3) & ~(int64_t)3) : 0u;
+            next_off = lane * 4;
         } else if (wave == XL) {
             const int64_t blocks = (g.d_out + kBlock8 - 1) / kBlock8 - o0 / kBlock8;
             const uint64_t first = reinterpret_cast<uint64_t>(g.w.scales) + (uint64_t)(o0 / kBlock8 * g.w.ld_scales) * SIZE;
-            base = first & ~(uint64_t)3, base_step = 0, range = 0x7FFFFFFFu;
-            off = lane < S::BO / kBlock8 && lane < blocks ? (uint32_t)(first & 3) + (uint32_t)(lane * g.w.ld_scales) * SIZE : 0x80000000u;
-            off_step = SIZE, to = lds + S::XS_BYTES, stage_bytes = S::SCALES;
-        } else {
-            base = reinterpret_cast<uint64_t>(g.x.scales), base_step = 0, range = 0, off = 0x80000000u, off_step = 0, to = idle, stage_bytes = 0;
+            base = first & ~(uint64_t)3, range = 0x7FFFFFFFu;
+            if (lane < S::BO / kBlock8 && lane < blocks) next_off = (uint32_t)(first & 3) + (uint32_t)(lane * g.w.ld_scales) * SIZE;
         }
-        // (the same in every lane; saying so keeps them in scalar registers)
-        base = scalar((uint32_t)base) | (uint64_t)scalar((uint32_t)(base >> 32)) << 32, base_step = scalar((uint32_t)base_step) | (uint64_t)scalar((uint32_t)(base_step >> 32)) << 32;
-        range = scalar(range), to = scalar(to), off_step = scalar(off_step), stage_bytes = scalar(stage_bytes);
-        asm volatile("s_nop 4" : "+s"(base), "+s"(range), "+s"(to));  // (as settle)
+        next = {scalar(base), scalar(there ? range : 0u)};
     }
-    static __device__ __forceinline__ uint32_t scalar(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
-    __device__ __forceinline__ void load(int stage, bool live) {
-        const u32x4_t rsrc = {(uint32_t)base, (uint32_t)(base >> 32), live ? range : 0u, 0x00020000u};
-        load_dwords_to_lds(rsrc, to + (uint32_t)stage * stage_bytes, off & ~3u);
-        base += base_step, off += off_step;
+    __device__ __forceinline__ void turn(bool yes) {
+        at.base = yes ? next.base : at.base, at.range = yes ? next.range : at.range, off = yes ? next_off : off;
+    }
+    __device__ __forceinline__ void load(uint32_t stage) {
+        load_dwords_to_lds(at.descriptor(), to + stage * stage_bytes, off & ~3u);
+        at.base += base_step, off += off_step;
     }
 };
 
@@ -126,14 +139,15 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
     const int wt = wave / S::NO, wo = wave % S::NO, i16 = lane & 15, g4 = lane >> 4;
     // Work-groups are dealt round-robin to the 8 XCDs, each with an L2 of its own: one XCD gets a run of consecutive positions, and
     // positions go through bands of eight tile rows (tokens), column by column, so that what runs on an XCD shares rows of both.
-    const uint32_t tiles_t = (uint32_t)((g.n + BT - 1) / BT), tiles_o = (uint32_t)((g.d_out + BO - 1) / BO);
-    int64_t t0, o0;
-    {
-        const uint32_t blocks = gridDim.x, per = blocks / 8, rem = blocks % 8, x = blockIdx.x % 8, r = blockIdx.x / 8;
-        const uint32_t tile = x * per + (x < rem ? x : rem) + r, band = tile / (8 * tiles_o), in = tile - band * 8 * tiles_o;
+    // A work-group takes every so many-th position of its XCD's run, and requests the first steps of its next tile under the last ones
+    // of this: no tile but the first waits for its operands, and the results are on their way to memory under the next tile's MFMAs.
+    const uint32_t tiles_t = (uint32_t)((g.n + BT - 1) / BT), tiles_o = (uint32_t)((g.d_out + BO - 1) / BO), tiles = tiles_t * tiles_o;
+    const uint32_t xcd = blockIdx.x % 8, turns = (gridDim.x - xcd + 7) / 8, first = xcd * (tiles / 8) + min(xcd, tiles % 8), count = tiles / 8 + (xcd < tiles % 8);
+    auto tile_at = [&](uint32_t position, int64_t &t0, int64_t &o0) {
+        const uint32_t tile = first + position, band = tile / (8 * tiles_o), in = tile - band * 8 * tiles_o;
         const uint32_t rows = min(8u, tiles_t - band * 8), col = in / rows;
-        t0 = (int64_t)(band * 8 + in - col * rows) * BT, o0 = (int64_t)col * BO;
-    }
+        t0 = (int64_t)scalar(band * 8 + in - col * rows) * BT, o0 = (int64_t)scalar(col) * BO;
+    };
     const int steps = (int)((g.d_in + kBlock8 - 1) / kBlock8);
 
     typedef __attribute__((address_space(3))) unsigned char *lds_ptr_t;
@@ -141,34 +155,47 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
     Loads8<S::JX> lx;
     Loads8<S::JW> lw;
     ScaleLoads8<S, SCALE> ls;
-    lx.init(g.x.data + t0 * g.x.ld, g.x.ld, min((int64_t)BT, g.n - t0), g.d_in, lds0, wave, lane,
-            [](int r) { return (int64_t)(r / S::WT * S::WT + r % 16 * TJ + r % S::WT / 16); });
-    lw.init(g.w.data + o0 * g.w.ld, g.w.ld, min((int64_t)BO, g.d_out - o0), g.d_in, lds0 + S::X_BYTES, wave, lane,
-            [](int r) { return (int64_t)(r / 32 * 32 + r % 16 / 4 * 8 + r / 16 % 2 * 4 + r % 4); });
-    ls.init(g, t0, o0, lds0 + 2 * S::STAGE, lds0 + 2 * S::STAGE + 2 * S::SCALES, wave, lane);
-    // The step that is being requested, and the stage (as bytes) it goes to.
-    int asked = 0;
-    uint32_t soff = 0, last = 0, into = 0;
-    bool live = true;
-    auto begin = [&](int step, uint32_t stage) {
-        live = step < steps, soff = (uint32_t)step * 128u, last = step == steps - 1 ? 0xFFFFFFFFu : 0u, into = stage;
-        lx.rsrc[2] = live ? lx.range : 0u, lw.rsrc[2] = live ? lw.range : 0u;
+    lx.init(g.x.ld, g.d_in, lds0, wave, lane, [](int r) { return r / S::WT * S::WT + r % 16 * TJ + r % S::WT / 16; });
+    lw.init(g.w.ld, g.d_in, lds0 + S::X_BYTES, wave, lane, [](int r) { return r / 32 * 32 + r % 16 / 4 * 8 + r / 16 % 2 * 4 + r % 4; });
+    ls.init(g, lds0 + S::STAGES * S::STAGE, lds0 + S::STAGES * (S::STAGE + S::SCALES), wave);
+    // The tile whose operands are requested after the one that is being requested.
+    Span next_x, next_w;
+    int64_t next_t0 = 0, next_o0 = 0;
+    auto place = [&](uint32_t position) {
+        const bool there = position < count;
+        tile_at(there ? position : 0u, next_t0, next_o0);
+        next_x = rows_of(g.x, next_t0, min((int64_t)BT, g.n - next_t0), there);
+        next_w = rows_of(g.w, next_o0, min((int64_t)BO, g.d_out - next_o0), there);
+        ls.place(g, next_t0, next_o0, there, wave, lane);
+        asm volatile("s_nop 4" : "+s"(next_x.base), "+s"(next_x.range), "+s"(next_w.base), "+s"(next_w.range), "+s"(ls.next.base), "+s"(ls.next.range));  // (as settle)
+    };
+    // The step that is being requested, and the stage it goes to.
+    int asked = steps - 1;
+    uint32_t soff = 0, last = 0, into = S::STAGES - 1;
+    auto begin = [&] {
+        const bool turn = asked == steps - 1;
+        asked = turn ? 0 : asked + 1, into = into == S::STAGES - 1 ? 0 : into + 1;
+        lx.at.base = turn ? next_x.base : lx.at.base, lx.at.range = turn ? next_x.range : lx.at.range;
+        lw.at.base = turn ? next_w.base : lw.at.base, lw.at.range = turn ? next_w.range : lw.at.range;
+        ls.turn(turn);
+        soff = (uint32_t)asked * 128u, last = asked == steps - 1 ? 0xFFFFFFFFu : 0u;
     };
     auto load = [&](int i) {  // load i of that step: the scales first
         if (i == 0)
-            ls.load(into != 0, live);
+            ls.load(into);
         else if (i <= S::JX)
-            lx.load(i - 1, into, soff, last);
+            lx.load(i - 1, into * S::STAGE, soff, last);
         else
-            lw.load(i - 1 - S::JX, into, soff, last);
+            lw.load(i - 1 - S::JX, into * S::STAGE, soff, last);
     };
 
-    // A lane's place in a tile of 16 rows: row i16, chunks g4 and g4 + 4; `from`: the stage that is read (as bytes).
+    // A lane's place in a tile of 16 rows: row i16, chunks g4 and g4 + 4; `from`: the stage that is read.
     const uint32_t at0 = (uint32_t)(i16 * 128 + ((g4 ^ ((i16 >> 1) & 7)) << 4)), at1 = at0 ^ 64u;
     uint32_t from = 0, x0 = at0 + wt * S::WT * 128, x1 = at1 + wt * S::WT * 128, w0 = at0 + S::X_BYTES + wo * S::WO * 128, w1 = at1 + S::X_BYTES + wo * S::WO * 128;
-    auto turn_to = [&](uint32_t stage) {
-        const uint32_t by = stage - from;
-        from = stage, x0 += by, x1 += by, w0 += by, w1 += by;
+    auto turn_stage = [&] {
+        const bool around = from == S::STAGES - 1;
+        const uint32_t by = around ? 0u - (uint32_t)((S::STAGES - 1) * S::STAGE) : (uint32_t)S::STAGE;
+        from = around ? 0 : from + 1, x0 += by, x1 += by, w0 += by, w1 += by;
     };
     auto fragment = [&](uint32_t a, uint32_t b, int tile) {
         union {
@@ -181,18 +208,15 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
     };
 
     f32x4_t acc[TU][TJ];
-#pragma unroll
-    for (int u = 0; u < TU; ++u)
-#pragma unroll
-        for (int j = 0; j < TJ; ++j) acc[u][j] = (f32x4_t){0, 0, 0, 0};
     i32x8_t xf[TJ], wf[4];
     // Scales of a step, as read and as used: powers of two as bytes for the matrix instruction, or the products of X's and W's.
     constexpr int XS = SCALE == SCALE_F32 ? TJ : TJ / 4;
     uint32_t xs_read[XS], ws_read, xs[IN_MFMA ? XS : 1], ws = 0;
     float fs[IN_MFMA ? 1 : TJ];
-    uint32_t w_byte = (uint32_t)reinterpret_cast<uint64_t>(g.w.scales) + (uint32_t)((o0 + wo * S::WO) / kBlock8 * g.w.ld_scales);  // (of the step's scale)
+    uint32_t w_byte = 0;  // address of the step's scale of W
+    auto w_byte_of = [&](int64_t o0) { return (uint32_t)reinterpret_cast<uint64_t>(g.w.scales) + (uint32_t)((o0 + wo * S::WO) / kBlock8 * g.w.ld_scales); };
     auto read_scales = [&] {
-        const unsigned char *at = lds + 2 * S::STAGE + (from != 0 ? S::SCALES : 0);
+        const unsigned char *at = lds + S::STAGES * S::STAGE + from * S::SCALES;
         ws_read = *reinterpret_cast<const uint32_t *>(at + S::XS_BYTES + wo * S::WO / kBlock8 * 4);
 #pragma unroll
         for (int q = 0; q < XS; ++q) xs_read[q] = *reinterpret_cast<const uint32_t *>(at + (wt * S::WT + i16 * TJ) * (SCALE == SCALE_F32 ? 4 : 1) + 4 * q);
@@ -222,23 +246,34 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
 
     constexpr int TAIL = PD * TJ;  // MFMAs behind the barrier
     constexpr int LOADS = S::LOADS;
-    begin(0, 0);
+    constexpr int STORES = TJ * TU / 2;  // of a wave, at least, where the tile has all its rows and columns
+    constexpr int AHEAD = (S::STAGES - 2) * LOADS;  // behind the loads of the next step
+    static_assert((S::STAGES - 1) * LOADS <= 63 && AHEAD + STORES <= 63, "what a wait can count");
+    uint32_t position = blockIdx.x / 8;
+    place(position);
+    int64_t t0 = next_t0, o0 = next_o0;
+    begin();
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) load(i);
-    begin(1, S::STAGE);
-    constexpr int EARLY = [] {
-        int c = 0;
-        for (int i = 0; i < LOADS; ++i) c += i * S::SPAN / LOADS < TAIL ? 1 : 0;
-        return c;
-    }();
+    place(position + turns);
 #pragma unroll
-    for (int i = 0; i < EARLY; ++i) load(i);
-    wait_for_loads<EARLY>();
+    for (int k = 1; k < S::STAGES; ++k) {
+        begin();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(i);
+    }
+    wait_for_loads<(S::STAGES - 1) * LOADS>();
     __syncthreads();
     read_first();
     read_scales();
+    w_byte = w_byte_of(o0);
     take_scales();
-    asked = 1;
+
+    for (bool stored = false;;) {
+#pragma unroll
+    for (int u = 0; u < TU; ++u)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) acc[u][j] = (f32x4_t){0, 0, 0, 0};
 
     // Step by step: the first fragments and the scales are in registers.  A fragment of X gives its place to the next step's
     // behind its last use, so that one set is enough.
@@ -247,7 +282,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
             // The chunk of 16 that the contraction ends in: what lies behind the end becomes zeros, in LDS.
             const int c = (int)(g.d_in % kBlock8) / 16;
             for (int row = tid; row < BT + BO; row += S::THREADS) {
-                uint4 *at = reinterpret_cast<uint4 *>(lds + from + row * 128 + ((c ^ ((row >> 1) & 7)) << 4));
+                uint4 *at = reinterpret_cast<uint4 *>(lds + from * S::STAGE + row * 128 + ((c ^ ((row >> 1) & 7)) << 4));
                 *at = first_bytes(*at, g.d_in % 16);
             }
             __syncthreads();
@@ -264,14 +299,17 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
         for_each<S::MFMAS + (IN_MFMA ? 0 : 2)>([&](auto index) __attribute__((always_inline)) {
             constexpr int i = decltype(index)::value, u = i / TJ, j = i % TJ, q = i - (TU - PD) * TJ, slot = q >= 0 ? q : i + TAIL;
             if constexpr (q == 0) {  // every fragment of W of this stage is in registers, the next step's data are there
-                wait_for_loads<0>();
+                if (stored && left > steps - (S::STAGES - 1))
+                    wait_for_loads<AHEAD + STORES>();  // (behind those loads the results of the tile before went out)
+                else
+                    wait_for_loads<AHEAD>();
                 __syncthreads();
-                begin(++asked, from);
-                turn_to(S::STAGE - from);
+                begin();
+                turn_stage();
             }
             if constexpr (i < S::MFMAS) {
                 if constexpr (IN_MFMA) {
-                    add_scaled_products<F8, j % 4, S::PER_SIMD != 1>(wf[u % 4], xf[j], acc[u][j], ws, xs[j / 4]);
+                    add_scaled_products<F8, j % 4>(wf[u % 4], xf[j], acc[u][j], ws, xs[j / 4]);
                 } else if constexpr (EXACT) {
                     if constexpr (j == 0)
 #pragma unroll
@@ -297,53 +335,64 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
             }
             if constexpr (i < S::MFMAS) __builtin_amdgcn_sched_barrier(0);
         });
+        if (left == 1) w_byte = w_byte_of(next_o0);
         take_scales();
     }
-    wait_for_loads<0>();
-    if constexpr (IN_MFMA) settle_sums<S::PER_SIMD != 1>(acc);
+    if constexpr (IN_MFMA) settle_sums(acc);
 
     // Tiles 2 v and 2 v + 1 hold outputs 32 v + 8 g4 .. + 7 of the lane's tokens.
+    const bool whole = t0 + BT <= g.n && o0 + BO <= g.d_out;
+    const int64_t token0 = t0 + wt * S::WT + i16 * TJ, out0 = o0 + wo * S::WO + 8 * g4;
+    // (token by token, so that its lines fill up at once: 16384 x 1024 -> 4096, 8 waves, 82 us with the tokens inside, 77 like this)
+    auto store = [&](int j, int v, bool checked) __attribute__((always_inline)) {
+        const int64_t o = out0 + 32 * v, valid = g.d_out - o;
+        float y[8];
 #pragma unroll
-    for (int v = 0; v < TU / 2; ++v) {
-        const int64_t o = o0 + wo * S::WO + 32 * v + 8 * g4, valid = g.d_out - o;
-        float b[8];
-        if (g.bias != nullptr) load8<T>((const T *)g.bias + (valid > 0 ? o : 0), valid, b);
+        for (int r = 0; r < 4; ++r) y[r] = acc[2 * v][j][r], y[4 + r] = acc[2 * v + 1][j][r];
+        if (checked && g.bias != nullptr) {  // (adding +0 would turn a -0 into +0: only where a bias exists)
+            float b[8];
+            load8<T>((const T *)g.bias + (valid > 0 ? o : 0), valid, b);
 #pragma unroll
-        for (int j = 0; j < TJ; ++j) {
-            const int64_t token = t0 + wt * S::WT + i16 * TJ + j;
-            float y[8];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = acc[2 * v][j][r], y[4 + r] = acc[2 * v + 1][j][r];
-            if (g.bias != nullptr)
-#pragma unroll
-                for (int r = 0; r < 8; ++r) y[r] += b[r];
-            if (token < g.n) store8<T>((T *)g.Y + token * g.d_out + (valid > 0 ? o : 0), valid, y);
+            for (int r = 0; r < 8; ++r) y[r] += b[r];
         }
+        if (!checked)
+            store8<T>((T *)g.Y + (token0 + j) * g.d_out + o, 8, y);
+        else if (token0 + j < g.n)
+            store8<T>((T *)g.Y + (token0 + j) * g.d_out + (valid > 0 ? o : 0), valid, y);
+    };
+    const bool checked = !whole || g.bias != nullptr;
+#pragma unroll
+    for (int j = 0; j < TJ; ++j)
+#pragma unroll
+        for (int v = 0; v < TU / 2; ++v) {
+            if (checked)
+                store(j, v, true);
+            else
+                store(j, v, false);
+        }
+    position += turns;
+    if (position >= count) break;
+    stored = whole;
+    t0 = next_t0, o0 = next_o0;
+    place(position + turns);
     }
+    wait_for_loads<0>();  // (of no tile: zeros, but into LDS that is another work-group's from here on)
 }
 
-// Which product takes which tile.
-typedef Tile8<256, 256, 2, 2, 3, 40, 1> Large8;   // 4 waves of 128 x 128, powers of two
-typedef Tile8<256, 256, 4, 2, 3, 20, 2> Eight8;   // 8 waves of 64 x 128, fp32 scales
-typedef Tile8<128, 128, 2, 2, 3, 12, 2> Mid8;     // 4 waves of 64 x 64
+typedef Tile8<256, 256, 4, 2, 2, 12, 2> Large8;   // 8 waves of 64 x 128
+typedef Tile8<128, 128, 2, 2, 2, 12, 2> Mid8;     // 4 waves of 64 x 64, two work-groups to a compute unit
 
 template <typename S, int F8, int SCALE, typename T>
 void launch_tile(const Linear8Args &g, hipStream_t stream) {
-    const unsigned tiles = (unsigned)((g.n + S::BT - 1) / S::BT * ((g.d_out + S::BO - 1) / S::BO));
+    const int64_t tiles = (g.n + S::BT - 1) / S::BT * ((g.d_out + S::BO - 1) / S::BO), places = 256 * (160 * 1024 / S::LDS_BYTES);
+    const int64_t steps = (g.d_in + kBlock8 - 1) / kBlock8;
+    const unsigned grid = (unsigned)(steps >= S::STAGES && tiles > places ? places : tiles);  // (requests reach into one further tile, no more)
     if (g.d_in % 16 != 0)
-        linear8_tile_kernel<S, F8, SCALE, T, true><<<tiles, S::THREADS, 0, stream>>>(g);
+        linear8_tile_kernel<S, F8, SCALE, T, true><<<grid, S::THREADS, 0, stream>>>(g);
     else
-        linear8_tile_kernel<S, F8, SCALE, T, false><<<tiles, S::THREADS, 0, stream>>>(g);
+        linear8_tile_kernel<S, F8, SCALE, T, false><<<grid, S::THREADS, 0, stream>>>(g);
 }
 
 }  // namespace
-
-template <int F8, int SCALE, typename T>
-void launch_linear8_tiles(const Linear8Args &g, bool large, hipStream_t stream) {
-    if constexpr (sizeof(T) == 2) {
-        if (large) return launch_tile<std::conditional_t<SCALE == SCALE_E8M0, Large8, Eight8>, F8, SCALE, T>(g, stream);
-    }
-    launch_tile<Mid8, F8, SCALE, T>(g, stream);
-}
 
 }  // namespace rmm
