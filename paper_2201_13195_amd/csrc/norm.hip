@@ -16,16 +16,11 @@ namespace {
 
 constexpr int kRun = 8;  // columns of a lane's run
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
-}
 // Sum over the WPR waves of a row, the same in all of them (red: two rows of WPR numbers, taken in turns so that one
 // barrier a row is enough).
 template <int WPR>
 __device__ __forceinline__ float row_sum(float v, float *red, int turn) {
-    v = wave_sum(v);
+    v = sum_of_64(v);
     if constexpr (WPR > 1) {
         float *to = red + (turn & 1) * WPR;
         if ((threadIdx.x & 63) == 0) to[threadIdx.x >> 6] = v;
@@ -81,31 +76,36 @@ __device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col
 }
 
 // h of eight columns, written to H if there is a residual.
-template <typename T>
-__device__ __forceinline__ void take_h(const NormArgs &g, int64_t row, int64_t col, float (&h)[8]) {
-    const int64_t at = row * g.d + (col < g.d ? col : 0), valid = g.d - col;
-    load8<T>((const T *)g.X + at, valid, h);
+template <typename T, bool EVEN>
+__device__ __forceinline__ void make_h(const NormArgs &g, int64_t at, int64_t valid, const Run8<T> &x, const Run8<T> &r, float (&h)[8]) {
+    x.get(h);
     if (g.residual != nullptr) {
-        float r[8];
-        load8<T>((const T *)g.residual + at, valid, r);
+        float f[8];
+        r.get(f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = rounded<T>(h[i] + r[i]);
-        if (g.H != nullptr) store8<T>((T *)g.H + at, valid, h);
+        for (int i = 0; i < 8; ++i) h[i] = rounded<T>(h[i] + f[i]);
+        if (g.H != nullptr) store_run<T, EVEN>((T *)g.H + at, valid, h);
     }
 }
 
-template <typename T, int CH, int WPR>
+template <typename T, int CH, int WPR, bool EVEN>
 __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_kernel(NormArgs g) {
     __shared__ float red[2 * WPR];
     const Place<WPR> p;
-    float w[CH][8];
+    Run8<T> w[CH];
 #pragma unroll
-    for (int c = 0; c < CH; ++c) load8<T>((const T *)g.weight + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c), w[c]);
+    for (int c = 0; c < CH; ++c) w[c] = load_run<T, EVEN>((const T *)g.weight + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c));
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * p.ROWS + p.row; row < g.n; row += (int64_t)gridDim.x * p.ROWS, ++turn) {
+        Run8<T> x[CH], r[CH];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) x[c] = load_run<T, EVEN>((const T *)g.X + row * g.d + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c));
+        if (g.residual != nullptr)
+#pragma unroll
+            for (int c = 0; c < CH; ++c) r[c] = load_run<T, EVEN>((const T *)g.residual + row * g.d + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c));
         float h[CH][8], sum = 0.0f;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) take_h<T>(g, row, p.col(c), h[c]);
+        for (int c = 0; c < CH; ++c) make_h<T, EVEN>(g, row * g.d + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c), x[c], r[c], h[c]);
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -115,15 +115,25 @@ __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_kernel(NormArgs 
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int64_t col = p.col(c);
+            float f[8];
+            w[c].get(f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * rstd * w[c][i];
-            if (g.Y != nullptr) store8<T>((T *)g.Y + row * g.d + (col < g.d ? col : 0), g.d - col, h[c]);
+            for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * rstd * f[i];
+            if (g.Y != nullptr) store_run<T, EVEN>((T *)g.Y + row * g.d + (col < g.d ? col : 0), g.d - col, h[c]);
             if (g.y8.data != nullptr) put8(g, row, col, p.lane, h[c]);
         }
     }
 }
 
 // Rows of any length, read twice (the second time mostly from L2).
+template <typename T>
+__device__ __forceinline__ void take_h(const NormArgs &g, int64_t row, int64_t col, float (&h)[8]) {
+    const int64_t at = row * g.d + (col < g.d ? col : 0), valid = g.d - col;
+    const Run8<T> x = load_run<T, false>((const T *)g.X + at, valid);
+    Run8<T> r;
+    if (g.residual != nullptr) r = load_run<T, false>((const T *)g.residual + at, valid);
+    make_h<T, false>(g, at, valid, x, r, h);
+}
 template <typename T>
 __global__ void __launch_bounds__(1024) rms_norm_long_kernel(NormArgs g) {
     __shared__ float red[2 * 16];
@@ -162,53 +172,81 @@ struct NormBackwardArgs {
     int64_t n, d;
 };
 
-template <typename T, int CH, int WPR>
+// What is read of a row; with up to four waves a row, that of the next row is requested before this one is reduced (16 waves are 128
+// registers each, and enough requests between them).
+template <typename T, int CH>
+struct BackwardRow {
+    Run8<T> dy[CH], h[CH], dh[CH];
+    float rstd;
+};
+template <typename T, int CH, int WPR, bool EVEN>
+__device__ __forceinline__ void load_row(BackwardRow<T, CH> &q, const NormBackwardArgs &g, const Place<WPR> &p, int64_t row) {
+    q.rstd = g.rstd[row];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int64_t at = row * g.d + (p.col(c) < g.d ? p.col(c) : 0), valid = g.d - p.col(c);
+        q.dy[c] = load_run<T, EVEN>((const T *)g.dY + at, valid);
+        q.h[c] = load_run<T, EVEN>((const T *)g.H + at, valid);
+    }
+    if (g.dH != nullptr)
+#pragma unroll
+        for (int c = 0; c < CH; ++c) q.dh[c] = load_run<T, EVEN>((const T *)g.dH + row * g.d + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c));
+}
+
+template <typename T, int CH, int WPR, bool EVEN>
 __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_backward_kernel(NormBackwardArgs g) {
     constexpr int PARKED = WPR == 1 ? 3 * CH * 64 * kRun : 1;  // dw of the waves that hold rows of their own
     __shared__ float red[2 * WPR];
     __shared__ float parked[PARKED];
     const Place<WPR> p;
     const float inv_d = 1.0f / (float)g.d;
-    float w[CH][8], dw[CH][8];
+    Run8<T> weight[CH];
+    float dw[CH][8];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        load8<T>((const T *)g.weight + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c), w[c]);
+        weight[c] = load_run<T, EVEN>((const T *)g.weight + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c));
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[c][i] = 0.0f;
     }
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * p.ROWS + p.row; row < g.n; row += (int64_t)gridDim.x * p.ROWS, ++turn) {
+    const int64_t step = (int64_t)gridDim.x * p.ROWS;
+    int64_t row = (int64_t)blockIdx.x * p.ROWS + p.row;
+    constexpr bool AHEAD = WPR < 16;
+    BackwardRow<T, CH> now, next;
+    if (AHEAD && row < g.n) load_row<T, CH, WPR, EVEN>(now, g, p, row);
+    for (int turn = 0; row < g.n; row += step, ++turn) {
+        if constexpr (!AHEAD)
+            load_row<T, CH, WPR, EVEN>(now, g, p, row);
+        else if (row + step < g.n)
+            load_row<T, CH, WPR, EVEN>(next, g, p, row + step);
         float dy[CH][8], h[CH][8], sum = 0.0f;
-        const float rstd = g.rstd[row];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int64_t col = p.col(c), at = row * g.d + (col < g.d ? col : 0);
-            load8<T>((const T *)g.dY + at, g.d - col, dy[c]);
-            load8<T>((const T *)g.H + at, g.d - col, h[c]);
-        }
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
+            float w[8];
+            now.dy[c].get(dy[c]), now.h[c].get(h[c]), weight[c].get(w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                h[c][i] *= rstd;
+                h[c][i] *= now.rstd;
                 dw[c][i] = fmaf(dy[c][i], h[c][i], dw[c][i]);
-                dy[c][i] *= w[c][i];
+                dy[c][i] *= w[i];
                 sum = fmaf(dy[c][i], h[c][i], sum);
             }
-        if (g.dX == nullptr) continue;  // (the same for all)
-        const float mean = row_sum<WPR>(sum, red, turn) * inv_d;
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int64_t col = p.col(c), at = row * g.d + (col < g.d ? col : 0);
-            float more[8];
-            if (g.dH != nullptr) load8<T>((const T *)g.dH + at, g.d - col, more);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float v = rstd * fmaf(-h[c][i], mean, dy[c][i]);
-                dy[c][i] = g.dH != nullptr ? v + more[i] : v;
-            }
-            store8<T>((T *)g.dX + at, g.d - col, dy[c]);
         }
+        if (g.dX != nullptr) {  // (the same for all)
+            const float mean = row_sum<WPR>(sum, red, turn) * inv_d;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int64_t col = p.col(c), at = row * g.d + (col < g.d ? col : 0);
+                float more[8];
+                if (g.dH != nullptr) now.dh[c].get(more);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float v = now.rstd * fmaf(-h[c][i], mean, dy[c][i]);
+                    dy[c][i] = g.dH != nullptr ? v + more[i] : v;
+                }
+                store_run<T, EVEN>((T *)g.dX + at, g.d - col, dy[c]);
+            }
+        }
+        if constexpr (AHEAD) now = next;
     }
     if (g.part == nullptr) return;
     if constexpr (WPR == 1) {  // the four waves' sums, in the order of the waves
@@ -320,7 +358,7 @@ __global__ void __launch_bounds__(1024) sum_parts_kernel(const float *__restrict
 constexpr int64_t columns(int ch, int wpr) { return (int64_t)ch * wpr * 64 * kRun; }
 int64_t rows_a_group(int64_t d) { return d <= columns(2, 1) ? 4 : 1; }
 constexpr int64_t kMostForward = 2048, kMostBackward = 512;  // work-groups: eight, two for each compute unit
-bool long_rows(int64_t d) { return d > columns(4, 16); }
+bool long_rows(int64_t d) { return d > columns(2, 16); }  // of the backward pass
 int64_t backward_groups(int64_t n, int64_t d) {
     if (long_rows(d)) return n < 16 ? n : 16;
     const int64_t groups = (n + rows_a_group(d) - 1) / rows_a_group(d);
@@ -328,6 +366,9 @@ int64_t backward_groups(int64_t n, int64_t d) {
 }
 
 }  // namespace
+
+#define LAUNCH(KERNEL, CH, WPR, THREADS) \
+    (d % 8 == 0 ? KERNEL<T, CH, WPR, true><<<grid, THREADS, 0, stream>>>(g) : KERNEL<T, CH, WPR, false><<<grid, THREADS, 0, stream>>>(g))
 
 size_t norm_backward_partials(int64_t n, int64_t d) { return (size_t)backward_groups(n, d) * (size_t)d; }
 
@@ -338,17 +379,17 @@ hipError_t launch_rms_norm(const T *X, const T *residual, const T *weight, T *H,
     const int64_t groups = (n + rows_a_group(d) - 1) / rows_a_group(d);
     const unsigned grid = (unsigned)(groups < kMostForward ? groups : kMostForward);
     if (d <= columns(1, 1))
-        rms_norm_kernel<T, 1, 1><<<grid, 256, 0, stream>>>(g);
+        LAUNCH(rms_norm_kernel, 1, 1, 256);
     else if (d <= columns(2, 1))
-        rms_norm_kernel<T, 2, 1><<<grid, 256, 0, stream>>>(g);
+        LAUNCH(rms_norm_kernel, 2, 1, 256);
     else if (d <= columns(1, 4))
-        rms_norm_kernel<T, 1, 4><<<grid, 256, 0, stream>>>(g);
+        LAUNCH(rms_norm_kernel, 1, 4, 256);
     else if (d <= columns(2, 4))
-        rms_norm_kernel<T, 2, 4><<<grid, 256, 0, stream>>>(g);
+        LAUNCH(rms_norm_kernel, 2, 4, 256);
     else if (d <= columns(4, 4))
-        rms_norm_kernel<T, 4, 4><<<grid, 256, 0, stream>>>(g);
+        LAUNCH(rms_norm_kernel, 4, 4, 256);
     else if (d <= columns(4, 16))
-        rms_norm_kernel<T, 4, 16><<<grid, 1024, 0, stream>>>(g);
+        LAUNCH(rms_norm_kernel, 4, 16, 1024);
     else
         rms_norm_long_kernel<T><<<grid, 1024, 0, stream>>>(g);
     return hipGetLastError();
@@ -365,17 +406,15 @@ hipError_t launch_rms_norm_backward(const T *dY, const T *dH, const T *H, const 
             rms_norm_dweight_kernel<T><<<dim3((unsigned)(wide < (1 << 20) ? wide : (1 << 20)), grid), 64, 0, stream>>>(g);
         if (dX != nullptr) rms_norm_backward_long_kernel<T><<<(unsigned)(n < kMostForward ? n : kMostForward), 1024, 0, stream>>>(g);
     } else if (d <= columns(1, 1)) {
-        rms_norm_backward_kernel<T, 1, 1><<<grid, 256, 0, stream>>>(g);
+        LAUNCH(rms_norm_backward_kernel, 1, 1, 256);
     } else if (d <= columns(2, 1)) {
-        rms_norm_backward_kernel<T, 2, 1><<<grid, 256, 0, stream>>>(g);
+        LAUNCH(rms_norm_backward_kernel, 2, 1, 256);
     } else if (d <= columns(1, 4)) {
-        rms_norm_backward_kernel<T, 1, 4><<<grid, 256, 0, stream>>>(g);
+        LAUNCH(rms_norm_backward_kernel, 1, 4, 256);
     } else if (d <= columns(2, 4)) {
-        rms_norm_backward_kernel<T, 2, 4><<<grid, 256, 0, stream>>>(g);
-    } else if (d <= columns(2, 16)) {
-        rms_norm_backward_kernel<T, 2, 16><<<grid, 1024, 0, stream>>>(g);
+        LAUNCH(rms_norm_backward_kernel, 2, 4, 256);
     } else {
-        rms_norm_backward_kernel<T, 4, 16><<<grid, 1024, 0, stream>>>(g);
+        LAUNCH(rms_norm_backward_kernel, 2, 16, 1024);
     }
     if (dweight != nullptr) {
         const int64_t wide = (d + 15) / 16;
@@ -383,6 +422,8 @@ hipError_t launch_rms_norm_backward(const T *dY, const T *dH, const T *H, const 
     }
     return hipGetLastError();
 }
+
+#undef LAUNCH
 
 #define INSTANCES(T)                                                                                                                 \
     template hipError_t launch_rms_norm<T>(const T *, const T *, const T *, T *, T *, const Mat8 *, int, int, float *, int64_t, int64_t, \

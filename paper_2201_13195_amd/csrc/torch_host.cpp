@@ -16,6 +16,7 @@
 #include <torch/csrc/autograd/saved_variable.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <ATen/ATen.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
 
 #include "../../include/rmm.h"
@@ -393,9 +394,14 @@ at::ScalarType arg_dtype(PyObject *o) {
 int64_t blocks8(int64_t d) { return (d + 127) / 128; }
 int64_t pitch16(int64_t d) { return (d + 15) / 16 * 16; }
 
+// New memory beside `like`, straight from the allocator: a call of these has up to five outputs, and the way through the dispatcher
+// is half a microsecond for each (a norm of one token 7.1 -> 6.0 us of host time, the launch among them).
+Tensor fresh(const Tensor &like, at::IntArrayRef sizes, at::ScalarType dtype) {
+    return Tensor(at::detail::empty_cuda(sizes, dtype, like.device(), c10::nullopt));
+}
 // rows x cols of a new buffer with rows of `pitch`.
 Tensor new_pitched(const Tensor &like, int64_t rows, int64_t cols, int64_t pitch, at::ScalarType dtype) {
-    Tensor t = at::empty({rows, pitch}, like.options().dtype(dtype).requires_grad(false));
+    Tensor t = fresh(like, {rows, pitch}, dtype);
     if (pitch != cols) t.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef{rows, cols}, at::IntArrayRef{pitch, 1});
     return t;
 }
@@ -484,7 +490,7 @@ PyObject *py_linear8(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     need(w.f8 == RMM_F8_E4M3 && w.scale == x.scale);
     const int64_t n = X.size(0), d_in = X.size(1), d_out = W.size(0);
     const c10::DeviceGuard guard(X.device());
-    if (!Y.defined()) Y = at::empty({n, d_out}, X.options().dtype(dtype).requires_grad(false));
+    if (!Y.defined()) Y = fresh(X, {n, d_out}, dtype);
     need(Y.scalar_type() == dtype && Y.device() == X.device() && is_matrix(Y, n, d_out, Y));
     need(!bias.defined() || is_matrix(bias, d_out, -1, Y));
     void *stream = current_stream(X);
@@ -514,8 +520,8 @@ PyObject *py_rms_norm(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
         need(f8_code(f8) >= 0 && scale_code(scale) >= 0);
         y8 = new_mat8(X, n, d, false, f8, scale);
     }
-    const Tensor H = residual.defined() ? new_matrix(X, n, d) : X, rstd = at::empty({n}, X.options().dtype(at::kFloat).requires_grad(false));
-    const Tensor Y = need_Y ? new_matrix(X, n, d) : Tensor();
+    const Tensor H = residual.defined() ? fresh(X, {n, d}, X.scalar_type()) : X, rstd = fresh(X, {n}, at::kFloat);
+    const Tensor Y = need_Y ? fresh(X, {n, d}, X.scalar_type()) : Tensor();
     void *stream = current_stream(X);
     int rc;
     {
@@ -538,8 +544,8 @@ PyObject *py_rms_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t nargs)
     need(rstd.is_cuda() && rstd.device() == dY.device() && rstd.scalar_type() == at::kFloat && rstd.is_contiguous() && rstd.dim() == 1 &&
          rstd.size(0) == n);
     const c10::DeviceGuard guard(dY.device());
-    const Tensor dX = need_dX ? new_matrix(dY, n, d) : Tensor(), dw = need_dw ? at::empty({d}, dY.options().requires_grad(false)) : Tensor();
-    const Tensor ws = need_dw ? scratch(dY, rmm_rms_norm_workspace_bytes(n, d, dtype_code(dY))) : Tensor();
+    const Tensor dX = need_dX ? fresh(dY, {n, d}, dY.scalar_type()) : Tensor(), dw = need_dw ? fresh(dY, {d}, dY.scalar_type()) : Tensor();
+    const Tensor ws = need_dw ? fresh(dY, {(int64_t)rmm_rms_norm_workspace_bytes(n, d, dtype_code(dY))}, at::kByte) : Tensor();
     void *stream = current_stream(dY);
     int rc;
     {
