@@ -18,14 +18,14 @@ constexpr int kRun = 8;  // columns of a lane's run
 
 // Sum over the WPR waves of a row, the same in all of them (red: two rows of WPR numbers, taken in turns so that one
 // barrier a row is enough).
-template <int WPR>
-__device__ __forceinline__ float row_sum(float v, float *red, int turn) {
+template <int WPR, typename F>
+__device__ __forceinline__ F row_sum(F v, F *red, int turn) {
     v = sum_of_64(v);
     if constexpr (WPR > 1) {
-        float *to = red + (turn & 1) * WPR;
+        F *to = red + (turn & 1) * WPR;
         if ((threadIdx.x & 63) == 0) to[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = 0.0f;
+        v = 0;
 #pragma unroll
         for (int i = 0; i < WPR; ++i) v += to[i];
     }
@@ -50,28 +50,50 @@ struct NormArgs {
     float *rstd;
     int64_t n, d;
     float eps;
+    double inv_d;
 };
 
-// Eight columns of y to 8 bits.
+// 1 / sqrt(mean + eps), from fp32 by a step of Newton's: `high` is its fp32 number, `low` what is missing.
+struct Rstd {
+    float high, low;
+};
+__device__ __forceinline__ Rstd rstd_of(double sum, const NormArgs &g) {
+    const double m = sum * g.inv_d + (double)g.eps;
+    const double r = (double)(1.0f / sqrtf((float)m)), s = r * (1.5 - 0.5 * m * r * r);
+    // (where m is zero, infinite, no number or too far out for fp32, its own root says what fp32 makes of it)
+    if (!(m >= 0x1p-120 && m < 0x1p120)) return {(float)(1.0 / sqrt(m)), 0.0f};
+    const float high = (float)s;
+    return {high, (float)(s - (double)high)};
+}
+
+// Eight columns of y = h rstd w to 8 bits.  An 8-bit number is decided by where y / s lies between two of the format's, and
+// is as far off as they are apart where y is off by little and crosses over: y is made to twice the bits of fp32 here, as y + low.
 template <int F8, int SCALE>
-__device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col, int lane, const float (&y)[8]) {
+__device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col, int lane, const float (&h)[8], const Rstd &r, const float (&w)[8]) {
+    float y[8], low[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float p = h[i] * r.high, p_low = fmaf(h[i], r.low, fmaf(h[i], r.high, -p));
+        const float v = p * w[i], v_low = fmaf(p_low, w[i], fmaf(p, w[i], -v));
+        y[i] = v + v_low, low[i] = v_low - (y[i] - v);
+    }
     const BlockScale s = block_scale<F8, SCALE>(max_of_16(amax8(y)));
     if (col < g.d) {
-        store8_bytes(g.y8.data + row * g.y8.ld + col, g.d - col, to_f8<F8, SCALE>(y, s));
+        store8_bytes(g.y8.data + row * g.y8.ld + col, g.d - col, to_f8<F8, SCALE>(y, low, s));
         if ((lane & 15) == 0) store_scale<SCALE>(g.y8.scales, col / kBlock8 * g.y8.ld_scales + row, s);
     }
 }
-__device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col, int lane, const float (&y)[8]) {
+__device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col, int lane, const float (&h)[8], const Rstd &r, const float (&w)[8]) {
     if (g.f8 == F8_E4M3) {
         if (g.scale == SCALE_F32)
-            put8<F8_E4M3, SCALE_F32>(g, row, col, lane, y);
+            put8<F8_E4M3, SCALE_F32>(g, row, col, lane, h, r, w);
         else
-            put8<F8_E4M3, SCALE_E8M0>(g, row, col, lane, y);
+            put8<F8_E4M3, SCALE_E8M0>(g, row, col, lane, h, r, w);
     } else {
         if (g.scale == SCALE_F32)
-            put8<F8_E5M2, SCALE_F32>(g, row, col, lane, y);
+            put8<F8_E5M2, SCALE_F32>(g, row, col, lane, h, r, w);
         else
-            put8<F8_E5M2, SCALE_E8M0>(g, row, col, lane, y);
+            put8<F8_E5M2, SCALE_E8M0>(g, row, col, lane, h, r, w);
     }
 }
 
@@ -90,7 +112,7 @@ __device__ __forceinline__ void make_h(const NormArgs &g, int64_t at, int64_t va
 
 template <typename T, int CH, int WPR, bool EVEN>
 __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_kernel(NormArgs g) {
-    __shared__ float red[2 * WPR];
+    __shared__ double red[2 * WPR];
     const Place<WPR> p;
     Run8<T> w[CH];
 #pragma unroll
@@ -110,17 +132,19 @@ __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_kernel(NormArgs 
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum = fmaf(h[c][i], h[c][i], sum);
-        const float rstd = 1.0f / sqrtf(row_sum<WPR>(sum, red, turn) / (float)g.d + g.eps);
-        if (g.rstd != nullptr && p.part == 0 && p.lane == 0) g.rstd[row] = rstd;
+        const Rstd rstd = rstd_of(row_sum<WPR>((double)sum, red, turn), g);
+        if (g.rstd != nullptr && p.part == 0 && p.lane == 0) g.rstd[row] = rstd.high;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int64_t col = p.col(c);
             float f[8];
             w[c].get(f);
+            if (g.y8.data != nullptr) put8(g, row, col, p.lane, h[c], rstd, f);
+            if (g.Y != nullptr) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * rstd * f[i];
-            if (g.Y != nullptr) store_run<T, EVEN>((T *)g.Y + row * g.d + (col < g.d ? col : 0), g.d - col, h[c]);
-            if (g.y8.data != nullptr) put8(g, row, col, p.lane, h[c]);
+                for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * rstd.high * f[i];
+                store_run<T, EVEN>((T *)g.Y + row * g.d + (col < g.d ? col : 0), g.d - col, h[c]);
+            }
         }
     }
 }
@@ -136,7 +160,7 @@ __device__ __forceinline__ void take_h(const NormArgs &g, int64_t row, int64_t c
 }
 template <typename T>
 __global__ void __launch_bounds__(1024) rms_norm_long_kernel(NormArgs g) {
-    __shared__ float red[2 * 16];
+    __shared__ double red[2 * 16];
     const Place<16> p;
     int turn = 0;
     for (int64_t row = blockIdx.x; row < g.n; row += gridDim.x, ++turn) {
@@ -146,8 +170,8 @@ __global__ void __launch_bounds__(1024) rms_norm_long_kernel(NormArgs g) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum = fmaf(h[i], h[i], sum);
         }
-        const float rstd = 1.0f / sqrtf(row_sum<16>(sum, red, turn) / (float)g.d + g.eps);
-        if (g.rstd != nullptr && threadIdx.x == 0) g.rstd[row] = rstd;
+        const Rstd rstd = rstd_of(row_sum<16>((double)sum, red, turn), g);
+        if (g.rstd != nullptr && threadIdx.x == 0) g.rstd[row] = rstd.high;
         NormArgs again = g;  // (what was written is read back, by the thread that wrote it; the buffer may be that of X)
         if (g.residual != nullptr && g.H != nullptr) again.X = g.H, again.residual = nullptr;
         again.H = nullptr;
@@ -156,10 +180,12 @@ __global__ void __launch_bounds__(1024) rms_norm_long_kernel(NormArgs g) {
             float w[8];
             take_h<T>(again, row, col, h);
             load8<T>((const T *)g.weight + (col < g.d ? col : 0), g.d - col, w);
+            if (g.y8.data != nullptr) put8(g, row, col, p.lane, h, rstd, w);
+            if (g.Y != nullptr) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[i] = h[i] * rstd * w[i];
-            if (g.Y != nullptr) store8<T>((T *)g.Y + row * g.d + (col < g.d ? col : 0), g.d - col, h);
-            if (g.y8.data != nullptr) put8(g, row, col, p.lane, h);
+                for (int i = 0; i < 8; ++i) h[i] = h[i] * rstd.high * w[i];
+                store8<T>((T *)g.Y + row * g.d + (col < g.d ? col : 0), g.d - col, h);
+            }
         }
     }
 }
@@ -375,7 +401,7 @@ size_t norm_backward_partials(int64_t n, int64_t d) { return (size_t)backward_gr
 template <typename T>
 hipError_t launch_rms_norm(const T *X, const T *residual, const T *weight, T *H, T *Y, const Mat8 *Y8, int f8, int scale, float *rstd,
                            int64_t n, int64_t d, float eps, hipStream_t stream) {
-    const NormArgs g = {X, residual, weight, H, Y, Y8 != nullptr ? *Y8 : Mat8{nullptr, 0, nullptr, 0}, f8, scale, rstd, n, d, eps};
+    const NormArgs g = {X, residual, weight, H, Y, Y8 != nullptr ? *Y8 : Mat8{nullptr, 0, nullptr, 0}, f8, scale, rstd, n, d, eps, 1.0 / (double)d};
     const int64_t groups = (n + rows_a_group(d) - 1) / rows_a_group(d);
     const unsigned grid = (unsigned)(groups < kMostForward ? groups : kMostForward);
     if (d <= columns(1, 1))

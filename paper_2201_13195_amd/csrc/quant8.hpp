@@ -189,12 +189,19 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t amax_bits) {
 // v / s, correctly rounded.  A power of two: the product with its inverse is exact.  Else from q = v inv, which is a unit
 // or so off, and the remainder v - q s, which is exact in one fused operation: three instructions where the division
 // written out is ten (the norm's kernel would be bound by them).  (With s of 2^-90 and less the remainder could be below the
-// numbers of fp32, and an s that is no number has none: `slow`.)
+// numbers of fp32, and an s that is no number has none: `slow`.)  With a v that is known to more than fp32, as v + low, the
+// remainder takes what fp32 does not hold.
 template <int SCALE>
 __device__ __forceinline__ float over_scale(float v, const BlockScale &b) {
     const float q = v * b.inv;
     if constexpr (SCALE == SCALE_E8M0) return q;
     return fmaf(fmaf(-q, b.s, v), b.inv, q);
+}
+template <int SCALE>
+__device__ __forceinline__ float over_scale(float v, float low, const BlockScale &b) {
+    const float q = v * b.inv;
+    if constexpr (SCALE == SCALE_E8M0) return q;
+    return fmaf(fmaf(-q, b.s, v) + low, b.inv, q);
 }
 template <int F8>
 __device__ __forceinline__ uint32_t pack4_f8(float a, float b, float c, float d) {
@@ -204,6 +211,18 @@ __device__ __forceinline__ uint32_t pack4_f8(float a, float b, float c, float d)
     else
         r = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, 0, false), r = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, r, true);
     return (uint32_t)r;
+}
+template <int F8, int SCALE>
+__device__ __forceinline__ uint2 to_f8(const float (&v)[8], const float (&low)[8], const BlockScale &b) {
+    float q[8];
+    if (b.slow) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = v[i] / b.s;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = over_scale<SCALE>(v[i], low[i], b);
+    }
+    return make_uint2(pack4_f8<F8>(q[0], q[1], q[2], q[3]), pack4_f8<F8>(q[4], q[5], q[6], q[7]));
 }
 template <int F8, int SCALE>
 __device__ __forceinline__ uint2 to_f8(const float (&v)[8], const BlockScale &b) {
@@ -243,8 +262,19 @@ __device__ __forceinline__ float plus_lane(float v) {
     return v + __uint_as_float(from_lane<CTRL>(__float_as_uint(v)));
 }
 __device__ __forceinline__ float lane_value(float v, int lane) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane)); }
+template <int CTRL>
+__device__ __forceinline__ double plus_lane(double v) {
+    const uint64_t u = (uint64_t)__double_as_longlong(v);
+    return v + __longlong_as_double((long long)(from_lane<CTRL>((uint32_t)u) | (uint64_t)from_lane<CTRL>((uint32_t)(u >> 32)) << 32));
+}
+__device__ __forceinline__ double lane_value(double v, int lane) {
+    const uint64_t u = (uint64_t)__double_as_longlong(v);
+    return __longlong_as_double((long long)((uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane) |
+                                            (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane) << 32));
+}
 // Sum over the 64 lanes, the same in all.
-__device__ __forceinline__ float sum_of_64(float v) {
+template <typename F>
+__device__ __forceinline__ F sum_of_64(F v) {
     v = plus_lane<LANE_MIRROR16>(plus_lane<LANE_MIRROR8>(plus_lane<LANE_XOR2>(plus_lane<LANE_XOR1>(v))));
     return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
 }
