@@ -98,36 +98,36 @@ __device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col
 }
 
 // h of eight columns, written to H if there is a residual.
-template <typename T, bool EVEN>
-__device__ __forceinline__ void make_h(const NormArgs &g, int64_t at, int64_t valid, const Run8<T> &x, const Run8<T> &r, float (&h)[8]) {
-    x.get(h);
+template <typename T, int MODE>
+__device__ __forceinline__ void make_h(const NormArgs &g, int64_t row, int64_t col, const Run8<T> &x, const Run8<T> &r, float (&h)[8]) {
+    values<T, MODE>(x, col, g.d, h);
     if (g.residual != nullptr) {
         float f[8];
-        r.get(f);
+        values<T, MODE>(r, col, g.d, f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[i] = rounded<T>(h[i] + f[i]);
-        if (g.H != nullptr) store_run<T, EVEN>((T *)g.H + at, valid, h);
+        if (g.H != nullptr) store_run<T, MODE>((T *)g.H + row * g.d, col, g.d, h);
     }
 }
 
-template <typename T, int CH, int WPR, bool EVEN>
+template <typename T, int CH, int WPR, int MODE>
 __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_kernel(NormArgs g) {
     __shared__ double red[2 * WPR];
     const Place<WPR> p;
     Run8<T> w[CH];
 #pragma unroll
-    for (int c = 0; c < CH; ++c) w[c] = load_run<T, EVEN>((const T *)g.weight + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c));
+    for (int c = 0; c < CH; ++c) w[c] = load_run<T, MODE>((const T *)g.weight, p.col(c), g.d);
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * p.ROWS + p.row; row < g.n; row += (int64_t)gridDim.x * p.ROWS, ++turn) {
         Run8<T> x[CH], r[CH];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) x[c] = load_run<T, EVEN>((const T *)g.X + row * g.d + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c));
+        for (int c = 0; c < CH; ++c) x[c] = load_run<T, MODE>((const T *)g.X + row * g.d, p.col(c), g.d);
         if (g.residual != nullptr)
 #pragma unroll
-            for (int c = 0; c < CH; ++c) r[c] = load_run<T, EVEN>((const T *)g.residual + row * g.d + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c));
+            for (int c = 0; c < CH; ++c) r[c] = load_run<T, MODE>((const T *)g.residual + row * g.d, p.col(c), g.d);
         float h[CH][8], sum = 0.0f;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) make_h<T, EVEN>(g, row * g.d + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c), x[c], r[c], h[c]);
+        for (int c = 0; c < CH; ++c) make_h<T, MODE>(g, row, p.col(c), x[c], r[c], h[c]);
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -138,12 +138,12 @@ __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_kernel(NormArgs 
         for (int c = 0; c < CH; ++c) {
             const int64_t col = p.col(c);
             float f[8];
-            w[c].get(f);
+            values<T, MODE>(w[c], col, g.d, f);
             if (g.y8.data != nullptr) put8(g, row, col, p.lane, h[c], rstd, f);
             if (g.Y != nullptr) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * rstd.high * f[i];
-                store_run<T, EVEN>((T *)g.Y + row * g.d + (col < g.d ? col : 0), g.d - col, h[c]);
+                store_run<T, MODE>((T *)g.Y + row * g.d, col, g.d, h[c]);
             }
         }
     }
@@ -152,11 +152,10 @@ __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_kernel(NormArgs 
 // Rows of any length, read twice (the second time mostly from L2).
 template <typename T>
 __device__ __forceinline__ void take_h(const NormArgs &g, int64_t row, int64_t col, float (&h)[8]) {
-    const int64_t at = row * g.d + (col < g.d ? col : 0), valid = g.d - col;
-    const Run8<T> x = load_run<T, false>((const T *)g.X + at, valid);
+    const Run8<T> x = load_run<T, ROWS_RAGGED>((const T *)g.X + row * g.d, col, g.d);
     Run8<T> r;
-    if (g.residual != nullptr) r = load_run<T, false>((const T *)g.residual + at, valid);
-    make_h<T, false>(g, at, valid, x, r, h);
+    if (g.residual != nullptr) r = load_run<T, ROWS_RAGGED>((const T *)g.residual + row * g.d, col, g.d);
+    make_h<T, ROWS_RAGGED>(g, row, col, x, r, h);
 }
 template <typename T>
 __global__ void __launch_bounds__(1024) rms_norm_long_kernel(NormArgs g) {
@@ -179,12 +178,12 @@ __global__ void __launch_bounds__(1024) rms_norm_long_kernel(NormArgs g) {
             const int64_t col = p.col(c);
             float w[8];
             take_h<T>(again, row, col, h);
-            load8<T>((const T *)g.weight + (col < g.d ? col : 0), g.d - col, w);
+            values<T, ROWS_RAGGED>(load_run<T, ROWS_RAGGED>((const T *)g.weight, col, g.d), col, g.d, w);
             if (g.y8.data != nullptr) put8(g, row, col, p.lane, h, rstd, w);
             if (g.Y != nullptr) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[i] = h[i] * rstd.high * w[i];
-                store8<T>((T *)g.Y + row * g.d + (col < g.d ? col : 0), g.d - col, h);
+                store_run<T, ROWS_RAGGED>((T *)g.Y + row * g.d, col, g.d, h);
             }
         }
     }
@@ -205,21 +204,20 @@ struct BackwardRow {
     Run8<T> dy[CH], h[CH], dh[CH];
     float rstd;
 };
-template <typename T, int CH, int WPR, bool EVEN>
+template <typename T, int CH, int WPR, int MODE>
 __device__ __forceinline__ void load_row(BackwardRow<T, CH> &q, const NormBackwardArgs &g, const Place<WPR> &p, int64_t row) {
     q.rstd = g.rstd[row];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int64_t at = row * g.d + (p.col(c) < g.d ? p.col(c) : 0), valid = g.d - p.col(c);
-        q.dy[c] = load_run<T, EVEN>((const T *)g.dY + at, valid);
-        q.h[c] = load_run<T, EVEN>((const T *)g.H + at, valid);
+        q.dy[c] = load_run<T, MODE>((const T *)g.dY + row * g.d, p.col(c), g.d);
+        q.h[c] = load_run<T, MODE>((const T *)g.H + row * g.d, p.col(c), g.d);
     }
     if (g.dH != nullptr)
 #pragma unroll
-        for (int c = 0; c < CH; ++c) q.dh[c] = load_run<T, EVEN>((const T *)g.dH + row * g.d + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c));
+        for (int c = 0; c < CH; ++c) q.dh[c] = load_run<T, MODE>((const T *)g.dH + row * g.d, p.col(c), g.d);
 }
 
-template <typename T, int CH, int WPR, bool EVEN>
+template <typename T, int CH, int WPR, int MODE>
 __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_backward_kernel(NormBackwardArgs g) {
     constexpr int PARKED = WPR == 1 ? 3 * CH * 64 * kRun : 1;  // dw of the waves that hold rows of their own
     __shared__ float red[2 * WPR];
@@ -230,7 +228,7 @@ __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_backward_kernel(
     float dw[CH][8];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        weight[c] = load_run<T, EVEN>((const T *)g.weight + (p.col(c) < g.d ? p.col(c) : 0), g.d - p.col(c));
+        weight[c] = load_run<T, MODE>((const T *)g.weight, p.col(c), g.d);
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[c][i] = 0.0f;
     }
@@ -238,17 +236,17 @@ __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_backward_kernel(
     int64_t row = (int64_t)blockIdx.x * p.ROWS + p.row;
     constexpr bool AHEAD = WPR < 16;
     BackwardRow<T, CH> now, next;
-    if (AHEAD && row < g.n) load_row<T, CH, WPR, EVEN>(now, g, p, row);
+    if (AHEAD && row < g.n) load_row<T, CH, WPR, MODE>(now, g, p, row);
     for (int turn = 0; row < g.n; row += step, ++turn) {
         if constexpr (!AHEAD)
-            load_row<T, CH, WPR, EVEN>(now, g, p, row);
+            load_row<T, CH, WPR, MODE>(now, g, p, row);
         else if (row + step < g.n)
-            load_row<T, CH, WPR, EVEN>(next, g, p, row + step);
+            load_row<T, CH, WPR, MODE>(next, g, p, row + step);
         float dy[CH][8], h[CH][8], sum = 0.0f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             float w[8];
-            now.dy[c].get(dy[c]), now.h[c].get(h[c]), weight[c].get(w);
+            values<T, MODE>(now.dy[c], p.col(c), g.d, dy[c]), values<T, MODE>(now.h[c], p.col(c), g.d, h[c]), values<T, MODE>(weight[c], p.col(c), g.d, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 h[c][i] *= now.rstd;
@@ -261,15 +259,15 @@ __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_backward_kernel(
             const float mean = row_sum<WPR>(sum, red, turn) * inv_d;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const int64_t col = p.col(c), at = row * g.d + (col < g.d ? col : 0);
+                const int64_t col = p.col(c);
                 float more[8];
-                if (g.dH != nullptr) now.dh[c].get(more);
+                if (g.dH != nullptr) values<T, MODE>(now.dh[c], col, g.d, more);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float v = now.rstd * fmaf(-h[c][i], mean, dy[c][i]);
                     dy[c][i] = g.dH != nullptr ? v + more[i] : v;
                 }
-                store_run<T, EVEN>((T *)g.dX + at, g.d - col, dy[c]);
+                store_run<T, MODE>((T *)g.dX + row * g.d, col, g.d, dy[c]);
             }
         }
         if constexpr (AHEAD) now = next;
@@ -306,31 +304,29 @@ __global__ void __launch_bounds__(1024) rms_norm_backward_long_kernel(NormBackwa
     for (int64_t row = blockIdx.x; row < g.n; row += gridDim.x, ++turn) {
         const float rstd = g.rstd[row];
         float dy[8], h[8], w[8], sum = 0.0f;
-        auto take = [&](int64_t col) {
-            const int64_t at = row * g.d + (col < g.d ? col : 0);
-            load8<T>((const T *)g.dY + at, g.d - col, dy);
-            load8<T>((const T *)g.H + at, g.d - col, h);
-            load8<T>((const T *)g.weight + (col < g.d ? col : 0), g.d - col, w);
+        auto take = [&](const void *from, int64_t col, float (&v)[8]) { values<T, ROWS_RAGGED>(load_run<T, ROWS_RAGGED>((const T *)from, col, g.d), col, g.d, v); };
+        auto take_both = [&](int64_t col) {
+            take((const T *)g.dY + row * g.d, col, dy), take((const T *)g.H + row * g.d, col, h), take(g.weight, col, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[i] *= rstd, dy[i] *= w[i];
         };
         for (int c = 0; p.col(c) < g.d; ++c) {
-            take(p.col(c));
+            take_both(p.col(c));
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum = fmaf(dy[i], h[i], sum);
         }
         const float mean = row_sum<16>(sum, red, turn) / (float)g.d;
         for (int c = 0; p.col(c) < g.d; ++c) {
-            const int64_t col = p.col(c), at = row * g.d + col;
+            const int64_t col = p.col(c);
             float more[8];
-            take(col);
-            if (g.dH != nullptr) load8<T>((const T *)g.dH + at, g.d - col, more);
+            take_both(col);
+            if (g.dH != nullptr) take((const T *)g.dH + row * g.d, col, more);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float v = rstd * fmaf(-h[i], mean, dy[i]);
                 dy[i] = g.dH != nullptr ? v + more[i] : v;
             }
-            store8<T>((T *)g.dX + at, g.d - col, dy);
+            store_run<T, ROWS_RAGGED>((T *)g.dX + row * g.d, col, g.d, dy);
         }
     }
 }
@@ -343,11 +339,10 @@ __global__ void __launch_bounds__(64) rms_norm_dweight_kernel(NormBackwardArgs g
         const int64_t col = c0 + threadIdx.x * kRun;
         float dw[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         for (int64_t row = blockIdx.y; row < g.n; row += gridDim.y) {
-            const int64_t at = row * g.d + (col < g.d ? col : 0);
             const float rstd = g.rstd[row];
             float dy[8], h[8];
-            load8<T>((const T *)g.dY + at, g.d - col, dy);
-            load8<T>((const T *)g.H + at, g.d - col, h);
+            values<T, ROWS_RAGGED>(load_run<T, ROWS_RAGGED>((const T *)g.dY + row * g.d, col, g.d), col, g.d, dy);
+            values<T, ROWS_RAGGED>(load_run<T, ROWS_RAGGED>((const T *)g.H + row * g.d, col, g.d), col, g.d, h);
 #pragma unroll
             for (int i = 0; i < 8; ++i) dw[i] = fmaf(dy[i], h[i] * rstd, dw[i]);
         }
@@ -393,8 +388,9 @@ int64_t backward_groups(int64_t n, int64_t d) {
 
 }  // namespace
 
+// (rows of fewer than eight columns are a kind of their own, of the smallest kernel alone)
 #define LAUNCH(KERNEL, CH, WPR, THREADS) \
-    (d % 8 == 0 ? KERNEL<T, CH, WPR, true><<<grid, THREADS, 0, stream>>>(g) : KERNEL<T, CH, WPR, false><<<grid, THREADS, 0, stream>>>(g))
+    (d % 8 == 0 ? KERNEL<T, CH, WPR, ROWS_EVEN><<<grid, THREADS, 0, stream>>>(g) : KERNEL<T, CH, WPR, ROWS_RAGGED><<<grid, THREADS, 0, stream>>>(g))
 
 size_t norm_backward_partials(int64_t n, int64_t d) { return (size_t)backward_groups(n, d) * (size_t)d; }
 
@@ -404,7 +400,9 @@ hipError_t launch_rms_norm(const T *X, const T *residual, const T *weight, T *H,
     const NormArgs g = {X, residual, weight, H, Y, Y8 != nullptr ? *Y8 : Mat8{nullptr, 0, nullptr, 0}, f8, scale, rstd, n, d, eps, 1.0 / (double)d};
     const int64_t groups = (n + rows_a_group(d) - 1) / rows_a_group(d);
     const unsigned grid = (unsigned)(groups < kMostForward ? groups : kMostForward);
-    if (d <= columns(1, 1))
+    if (d < 8)
+        rms_norm_kernel<T, 1, 1, ROWS_TINY><<<grid, 256, 0, stream>>>(g);
+    else if (d <= columns(1, 1))
         LAUNCH(rms_norm_kernel, 1, 1, 256);
     else if (d <= columns(2, 1))
         LAUNCH(rms_norm_kernel, 2, 1, 256);
@@ -431,6 +429,8 @@ hipError_t launch_rms_norm_backward(const T *dY, const T *dH, const T *H, const 
         if (dweight != nullptr)
             rms_norm_dweight_kernel<T><<<dim3((unsigned)(wide < (1 << 20) ? wide : (1 << 20)), grid), 64, 0, stream>>>(g);
         if (dX != nullptr) rms_norm_backward_long_kernel<T><<<(unsigned)(n < kMostForward ? n : kMostForward), 1024, 0, stream>>>(g);
+    } else if (d < 8) {
+        rms_norm_backward_kernel<T, 1, 1, ROWS_TINY><<<grid, 256, 0, stream>>>(g);
     } else if (d <= columns(1, 1)) {
         LAUNCH(rms_norm_backward_kernel, 1, 1, 256);
     } else if (d <= columns(2, 1)) {

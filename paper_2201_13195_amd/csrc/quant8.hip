@@ -11,7 +11,7 @@ constexpr int kRowsPerGroup = 16;  // rows of a work-group: 16 lanes each
 constexpr int kBlocksPerGroup = 4; // blocks of 128 columns, one after the other, all loaded first
 
 // Work-group (x, y): rows 16 x .., blocks 4 y ..  The 16 lanes of a row read 256 (bf16) or 512 consecutive bytes.
-template <typename T, int F8, int SCALE, bool EVEN>
+template <typename T, int F8, int SCALE, int MODE>
 __global__ void __launch_bounds__(256) quantize_rows8_kernel(const T *__restrict__ A, int64_t n, int64_t d, Mat8 out) {
     const int lane16 = threadIdx.x & 15;
     const int64_t row = (int64_t)blockIdx.x * kRowsPerGroup + (threadIdx.x >> 4);
@@ -22,17 +22,17 @@ __global__ void __launch_bounds__(256) quantize_rows8_kernel(const T *__restrict
 #pragma unroll
         for (int i = 0; i < kBlocksPerGroup; ++i) {
             const int64_t col = (b0 + i) * kBlock8 + lane16 * 8;
-            run[i] = load_run<T, EVEN>(A + row * d + (col < d ? col : 0), d - col);
+            run[i] = load_run<T, MODE>(A + row * d, col, d);
         }
 #pragma unroll
         for (int i = 0; i < kBlocksPerGroup; ++i) {
             if (b0 + i >= blocks) break;
             const int64_t col = (b0 + i) * kBlock8 + lane16 * 8;
             float v[8];
-            run[i].get(v);
+            values<T, MODE>(run[i], col, d, v);
             const BlockScale s = block_scale<F8, SCALE>(max_of_16(amax8(v)));
             const uint2 q = to_f8<F8, SCALE>(v, s);
-            if constexpr (EVEN) {
+            if constexpr (MODE == ROWS_EVEN) {
                 if (col < d) *reinterpret_cast<uint2 *>(out.data + row * out.ld + col) = q;
             } else {
                 store8_bytes(out.data + row * out.ld + col, d - col, q);
@@ -53,7 +53,7 @@ __device__ __forceinline__ void transpose_4x4(uint32_t (&a)[4]) {
 // A work-group for each 128 x 128 block: a thread holds 4 x 8 elements (rows 4 g .., columns 8 l ..).  The transposed bytes go through
 // LDS, four rows of a column at a time, and leave it as whole lines.  (8 x 8 elements a thread, written from registers in pieces of 8
 // bytes: 4096 x 1024 9.1 us, 768 x 768 7.9; like this 7.6 and 6.0.  A kernel of one row is 5 by the same clock.)
-template <typename T, int F8, int SCALE, bool EVEN>
+template <typename T, int F8, int SCALE, int MODE>
 __global__ void __launch_bounds__(512) quantize_weight8_kernel(const T *__restrict__ W, int64_t rows, int64_t cols, Mat8 out, Mat8 out_t) {
     __shared__ uint32_t most[8];
     // Column c: 32 dwords, dword g of four rows at position (g + 4 (c / 8)) % 32, so that neither side meets in the banks.
@@ -68,11 +68,11 @@ __global__ void __launch_bounds__(512) quantize_weight8_kernel(const T *__restri
         uint32_t m = 0;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const bool there = row0 + r < rows && col0 < cols;
-            run[r] = load_run<T, EVEN>(W + (there ? (row0 + r) * cols + col0 : 0), there ? cols - col0 : 0);
+            run[r] = load_run<T, MODE>(W + min(row0 + r, rows - 1) * cols, col0, cols);
         }
+        auto take = [&](int r) { values<T, MODE>(run[r], row0 + r < rows ? col0 : cols + 8, cols, v); };  // (rows that do not exist: zeros)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) run[r].get(v), m = max(m, amax8(v));
+        for (int r = 0; r < 4; ++r) take(r), m = max(m, amax8(v));
         m = max_of_16(m);
         const uint32_t m01 = max((uint32_t)__builtin_amdgcn_readlane((int)m, 0), (uint32_t)__builtin_amdgcn_readlane((int)m, 16));
         const uint32_t m23 = max((uint32_t)__builtin_amdgcn_readlane((int)m, 32), (uint32_t)__builtin_amdgcn_readlane((int)m, 48));
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(512) quantize_weight8_kernel(const T *__restri
         uint32_t q[2][4];  // [columns 0-3, 4-7][row]
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            run[r].get(v);
+            take(r);
             const uint2 p = to_f8<F8, SCALE>(v, s);
             q[0][r] = p.x, q[1][r] = p.y;
             if (row0 + r < rows && col0 < cols) store8_bytes(out.data + (row0 + r) * out.ld + col0, cols - col0, p);
@@ -118,7 +118,24 @@ __global__ void __launch_bounds__(512) quantize_weight8_kernel(const T *__restri
     }
 }
 
-// The four instances of a kernel template by format and kind of scale.
+template <typename T, int F8, int SCALE>
+void quantize_rows8(dim3 grid, const T *A, int64_t n, int64_t d, const Mat8 &out, hipStream_t stream) {
+    switch (rows_mode(d)) {
+        case ROWS_EVEN: quantize_rows8_kernel<T, F8, SCALE, ROWS_EVEN><<<grid, 256, 0, stream>>>(A, n, d, out); break;
+        case ROWS_RAGGED: quantize_rows8_kernel<T, F8, SCALE, ROWS_RAGGED><<<grid, 256, 0, stream>>>(A, n, d, out); break;
+        default: quantize_rows8_kernel<T, F8, SCALE, ROWS_TINY><<<grid, 256, 0, stream>>>(A, n, d, out);
+    }
+}
+template <typename T, int F8, int SCALE>
+void quantize_weight8(unsigned grid, const T *W, int64_t rows, int64_t cols, const Mat8 &out, const Mat8 &out_t, hipStream_t stream) {
+    switch (rows_mode(cols)) {
+        case ROWS_EVEN: quantize_weight8_kernel<T, F8, SCALE, ROWS_EVEN><<<grid, 512, 0, stream>>>(W, rows, cols, out, out_t); break;
+        case ROWS_RAGGED: quantize_weight8_kernel<T, F8, SCALE, ROWS_RAGGED><<<grid, 512, 0, stream>>>(W, rows, cols, out, out_t); break;
+        default: quantize_weight8_kernel<T, F8, SCALE, ROWS_TINY><<<grid, 512, 0, stream>>>(W, rows, cols, out, out_t);
+    }
+}
+
+// The four instances of a function template by format and kind of scale.
 #define RMM_BY_FORMAT(CALL)                                                                                             \
     (f8 == F8_E4M3 ? (scale == SCALE_F32 ? CALL(F8_E4M3, SCALE_F32) : CALL(F8_E4M3, SCALE_E8M0))                        \
                    : (scale == SCALE_F32 ? CALL(F8_E5M2, SCALE_F32) : CALL(F8_E5M2, SCALE_E8M0)))
@@ -134,10 +151,8 @@ hipError_t launch_quantize_rows8(const T *A, int64_t n, int64_t d, int f8, int s
         const int64_t row0 = g * kRowsPerGroup, here = groups - g < kMost ? groups - g : kMost;
         const int64_t width = (blocks + kBlocksPerGroup - 1) / kBlocksPerGroup, cut = width < 1024 ? width : 1024;
         const Mat8 o = {out.data + row0 * out.ld, out.ld, (char *)out.scales + row0 * (scale == SCALE_F32 ? 4 : 1), out.ld_scales};
-#define CALL(F, S)                                                                                                              \
-    (d % 8 == 0 ? (quantize_rows8_kernel<T, F, S, true><<<dim3((unsigned)here, (unsigned)cut), 256, 0, stream>>>(A + row0 * d, n - row0, d, o), 0) \
-                : (quantize_rows8_kernel<T, F, S, false><<<dim3((unsigned)here, (unsigned)cut), 256, 0, stream>>>(A + row0 * d, n - row0, d, o), 0))
-        (void)RMM_BY_FORMAT(CALL);
+#define CALL(F, S) quantize_rows8<T, F, S>(dim3((unsigned)here, (unsigned)cut), A + row0 * d, n - row0, d, o, stream)
+        RMM_BY_FORMAT(CALL);
 #undef CALL
     }
     return hipGetLastError();
@@ -149,10 +164,8 @@ hipError_t launch_quantize_weight8(const T *W, int64_t rows, int64_t cols, int f
     const int64_t blocks = ((rows + kBlock8 - 1) / kBlock8) * ((cols + kBlock8 - 1) / kBlock8);
     const unsigned grid = (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20));
     const Mat8 t = out_t != nullptr ? *out_t : Mat8{nullptr, 0, nullptr, 0};
-#define CALL(F, S)                                                                                                   \
-    (cols % 8 == 0 ? (quantize_weight8_kernel<T, F, S, true><<<grid, 512, 0, stream>>>(W, rows, cols, out, t), 0)    \
-                   : (quantize_weight8_kernel<T, F, S, false><<<grid, 512, 0, stream>>>(W, rows, cols, out, t), 0))
-    (void)RMM_BY_FORMAT(CALL);
+#define CALL(F, S) quantize_weight8<T, F, S>(grid, W, rows, cols, out, t, stream)
+    RMM_BY_FORMAT(CALL);
 #undef CALL
     return hipGetLastError();
 }

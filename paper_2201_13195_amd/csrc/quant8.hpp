@@ -62,47 +62,38 @@ __device__ __forceinline__ float rounded(float v) {
         return v;
 }
 
-// Eight consecutive elements, of which the first `valid` exist (others: 0), as they are in memory: loads of several runs, and of the
-// row that is next, are in flight before the first is waited for.  EVEN: rows of a multiple of eight, so that a run exists whole
-// or not at all, and no load stands behind a branch (with one, the compiler waits for each load where the branches meet: 768 x 768
-// weights to 8 bits 11.1 us, without 7.9).  Other rows start anywhere: the hardware takes 16-byte loads at any element's address.
+// Eight columns of a row, as they are in memory: the loads of several runs, and of the row that is next, are in flight before the
+// first is waited for.  So no load stands behind a branch (with one, the compiler waits for each load where the branches meet:
+// 768 x 768 weights to 8 bits 11.1 us, without 7.9), and what a run's end asks for happens when it is used.  Rows by their width:
+//   EVEN    a multiple of eight: a run exists whole or not at all
+//   RAGGED  eight and more: the run that the row ends in is loaded from eight before the end and shifted down (element by element
+//           behind a branch: norm backward of 16384 x 4095 bf16 214 us, like this 129)
+//   TINY    fewer: element by element
+// Rows start anywhere: the hardware takes 16-byte loads at any element's address.
+enum { ROWS_EVEN = 0, ROWS_RAGGED = 1, ROWS_TINY = 2 };
+inline int rows_mode(int64_t d) { return d % 8 == 0 ? ROWS_EVEN : d >= 8 ? ROWS_RAGGED : ROWS_TINY; }
 typedef uint32_t u32x4a_t __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4a_t __attribute__((ext_vector_type(4), aligned(4)));
 template <typename T>
 struct Run8 {
     uint32_t q[2 * sizeof(T)];
-    __device__ __forceinline__ void get(float (&v)[8]) const {
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(q[i] << 16), v[2 * i + 1] = __uint_as_float(q[i] & 0xFFFF0000u);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(q[i]);
-        }
-    }
 };
-// `p` may be read wherever valid <= 0 too.
-template <typename T, bool EVEN>
-__device__ __forceinline__ Run8<T> load_run(const T *p, int64_t valid) {
+// (also of columns that the row does not have)
+template <typename T, int MODE>
+__device__ __forceinline__ Run8<T> load_run(const T *row, int64_t col, int64_t d) {
     Run8<T> r;
-    auto whole = [&] {
+    if constexpr (MODE != ROWS_TINY) {
+        const T *p = row + (MODE == ROWS_EVEN ? (col < d ? col : 0) : min(col, d - 8));
 #pragma unroll
         for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
-            const u32x4a_t a = *reinterpret_cast<const u32x4a_t *>(p + 8 / (sizeof(T) / 2) * h);
+            const u32x4a_t a = *reinterpret_cast<const u32x4a_t *>(p + 16 / sizeof(T) * h);
 #pragma unroll
             for (int i = 0; i < 4; ++i) r.q[4 * h + i] = a[i];
         }
-    };
-    if constexpr (EVEN) {
-        whole();
-#pragma unroll
-        for (int i = 0; i < (int)(2 * sizeof(T)); ++i) r.q[i] = valid > 0 ? r.q[i] : 0u;
-    } else if (valid >= 8) {
-        whole();
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t e = i < valid ? __float_as_uint(load_f32<T>(p + i)) : 0u;
+            const uint32_t e = col + i < d ? __float_as_uint(load_f32<T>(row + col + i)) : 0u;
             if constexpr (sizeof(T) == 2)
                 r.q[i / 2] = i % 2 ? r.q[i / 2] | e : e >> 16;
             else
@@ -111,9 +102,42 @@ __device__ __forceinline__ Run8<T> load_run(const T *p, int64_t valid) {
     }
     return r;
 }
+// Its values as fp32; zeros where the row has no columns.
+template <typename T, int MODE>
+__device__ __forceinline__ void values(const Run8<T> &run, int64_t col, int64_t d, float (&v)[8]) {
+    constexpr int N = 2 * sizeof(T), A = N / 2;  // dwords, and those of four elements
+    uint32_t q[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) q[i] = run.q[i];
+    if constexpr (MODE == ROWS_EVEN) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) q[i] = col < d ? q[i] : 0u;
+    } else if constexpr (MODE == ROWS_RAGGED) {
+        const int by = (int)max((int64_t)0, min(col - (d - 8), (int64_t)8));  // elements
+#pragma unroll
+        for (int i = 0; i < N; ++i) q[i] = by & 4 ? (i + A < N ? q[i + A < N ? i + A : 0] : 0u) : q[i];
+#pragma unroll
+        for (int i = 0; i < N; ++i) q[i] = by & 2 ? (i + A / 2 < N ? q[i + A / 2 < N ? i + A / 2 : 0] : 0u) : q[i];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t above = i + 1 < N ? q[i + 1 < N ? i + 1 : 0] : 0u;
+            q[i] = by & 8 ? 0u : by & 1 ? (sizeof(T) == 2 ? q[i] >> 16 | above << 16 : above) : q[i];
+        }
+    }
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(q[i] << 16), v[2 * i + 1] = __uint_as_float(q[i] & 0xFFFF0000u);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(q[i]);
+    }
+}
 template <typename T>
 __device__ __forceinline__ void load8(const T *p, int64_t valid, float (&v)[8]) {
-    load_run<T, false>(p, valid).get(v);
+    if (valid >= 8)
+        values<T, ROWS_EVEN>(load_run<T, ROWS_EVEN>(p, 0, 8), 0, 8, v);
+    else
+        values<T, ROWS_TINY>(load_run<T, ROWS_TINY>(p, 0, valid), 0, valid, v);
 }
 template <typename T>
 __device__ __forceinline__ void store8(T *p, int64_t valid, const float (&v)[8]) {
@@ -133,12 +157,12 @@ __device__ __forceinline__ void store8(T *p, int64_t valid, const float (&v)[8])
             if (i < valid) store_f32<T>(p + i, v[i]);
     }
 }
-template <typename T, bool EVEN>
-__device__ __forceinline__ void store_run(T *p, int64_t valid, const float (&v)[8]) {
-    if constexpr (EVEN) {
-        if (valid > 0) store8<T>(p, 8, v);
+template <typename T, int MODE>
+__device__ __forceinline__ void store_run(T *row, int64_t col, int64_t d, const float (&v)[8]) {
+    if constexpr (MODE == ROWS_EVEN) {
+        if (col < d) store8<T>(row + col, 8, v);
     } else {
-        store8<T>(p, valid, v);
+        store8<T>(row + (col < d ? col : 0), d - col, v);
     }
 }
 // Eight data bytes to p (8-byte aligned), of which the first `valid` belong to the matrix.

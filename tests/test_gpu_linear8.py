@@ -4,6 +4,7 @@ import torch
 
 import eight
 import paper_2201_13195_amd as rmm
+from test_linear8_plan import KERNELS
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -47,6 +48,15 @@ SHAPES = [(1, 1, 1), (1, 128, 16), (1, 1000, 1111), (2, 129, 17), (7, 4096, 100)
 def test_shapes(n, d_in, d_out, scale_dtype):
     for f8, dtype, with_bias in ((E4, torch.bfloat16, True), (E5, torch.float32, False), (E4, torch.float32, True), (E5, torch.bfloat16, True)):
         x, w, bias = operands(n, d_in, d_out, f8, scale_dtype)
+        bias = bias.to(dtype).to(DEV) if with_bias else None
+        check(x, w, bias, dtype, rmm.rmm_linear8(*x, *w, bias=bias, dtype=dtype))
+
+
+@pytest.mark.parametrize("scale_dtype", eight.SCALES)
+@pytest.mark.parametrize("shape", [shape for shape, _, _ in KERNELS])
+def test_every_kernel(shape, scale_dtype):
+    for f8, dtype, with_bias in ((E4, torch.bfloat16, False), (E5, torch.bfloat16, True), (E4, torch.float32, True), (E5, torch.float32, False)):
+        x, w, bias = operands(*shape, f8, scale_dtype)
         bias = bias.to(dtype).to(DEV) if with_bias else None
         check(x, w, bias, dtype, rmm.rmm_linear8(*x, *w, bias=bias, dtype=dtype))
 

@@ -1,0 +1,82 @@
+"""CPU: which kernel a product of 8-bit operands takes (csrc/linear8_plan.hpp, compiled on the host)."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2201_13195_amd", "csrc")
+FEW_16x16, FEW_16x32, FEW_32x32, FEW_64x32, MANY_16x64, MANY_32x32, TILE_128, TILE_256 = range(8)
+UNITS = 256
+
+# (n, d_in, d_out) of each kernel, bf16 and fp32 results; tests/test_gpu_linear8.py runs them.
+KERNELS = [
+    ((5, 200, 70), FEW_16x16, FEW_16x16), ((256, 512, 256), FEW_16x16, FEW_16x16),
+    ((16, 1000, 5000), FEW_16x32, FEW_16x32), ((130, 777, 800), FEW_16x32, FEW_16x32),
+    ((60, 300, 3001), FEW_32x32, FEW_32x32), ((500, 900, 510), FEW_32x32, FEW_32x32),
+    ((333, 1000, 1111), FEW_64x32, FEW_64x32), ((128, 2048, 4000), FEW_64x32, FEW_64x32),
+    ((1, 520, 9001), MANY_16x64, MANY_16x64), ((16, 136, 20000), MANY_16x64, MANY_16x64),
+    ((20, 520, 9001), MANY_32x32, MANY_32x32), ((32, 131, 17000), MANY_32x32, MANY_32x32),
+    ((600, 400, 1200), TILE_128, TILE_128), ((1100, 2050, 1030), TILE_128, TILE_128),
+    ((2100, 250, 4100), TILE_128, TILE_128),          # more tiles than places, two steps: a work-group has a second tile
+    ((2100, 128, 4100), TILE_128, TILE_128),          # one step
+    ((4096, 1024, 4096), TILE_256, TILE_128), ((4300, 1000, 4090), TILE_256, TILE_128),      # (the second: two rounds of tiles)
+    ((5000, 512, 5000), TILE_256, TILE_128), ((9000, 384, 4104), TILE_256, TILE_128),
+]
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    where = tmp_path_factory.mktemp("plan")
+    src = where / "plan.cpp"
+    src.write_text('#include "linear8_plan.hpp"\nextern "C" int plan(int64_t n, int64_t d_in, int64_t d_out, int64_t x, int64_t w, bool exact) '
+                   "{ return rmm::linear8_plan(n, d_in, d_out, x, w, exact); }\n")
+    lib = str(where / "plan.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I" + CSRC,
+                    str(src), "-o", lib], check=True)
+    f = ctypes.CDLL(lib).plan
+    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_int64] * 5 + [ctypes.c_bool]
+    return lambda n, d_in, d_out, exact=False, x=None, w=None: f(n, d_in, d_out, x or (d_in + 15) // 16 * 16, w or (d_in + 15) // 16 * 16, exact)
+
+
+def groups(n, d_out, tokens, outputs):
+    return -(-n // tokens) * -(-d_out // outputs)
+
+
+@pytest.mark.parametrize("shape,bf16,f32", KERNELS)
+def test_kernels_by_shape(plan, shape, bf16, f32):
+    assert plan(*shape) == bf16 and plan(*shape, exact=True) == f32
+
+
+def test_every_kernel_is_among_them():
+    assert {k for _, k, _ in KERNELS} == set(range(8))
+
+
+def test_few_outputs_never_take_more_than_a_round(plan):
+    for n in (1, 2, 15, 16, 17, 31, 33, 64, 65, 100, 128, 200, 333, 512, 1000, 2048):
+        for d_out in (1, 16, 17, 100, 128, 700, 1024, 1111, 2048, 4096, 5000, 8192, 9000):
+            k = plan(n, 1024, d_out)
+            sizes = {FEW_16x16: (16, 16), FEW_16x32: (16, 32), FEW_32x32: (32, 32), FEW_64x32: (64, 32)}
+            if k in sizes:
+                assert groups(n, d_out, *sizes[k]) <= UNITS
+                assert all(groups(n, d_out, *sizes[j]) > UNITS for j in sizes if j < k)          # the smallest that does
+            else:
+                assert groups(n, d_out, 64, 32) > UNITS
+                assert (k == MANY_16x64) == (n <= 16) and (k == MANY_32x32) == (16 < n <= 32)
+
+
+def test_large_ones_take_the_large_tile(plan):
+    assert plan(16384, 4096, 4096) == plan(16384, 1024, 4096) == plan(16384, 4096, 1024) == TILE_256
+    assert plan(8192, 1024, 1024) == plan(4096, 768, 768) == plan(2048, 2048, 2048) == TILE_128
+    assert all(plan(n, d, d, exact=True) == TILE_128 for n in (2000, 20000) for d in (1000, 4096))
+
+
+def test_operands_beyond_32_bits_of_a_tile(plan):
+    """Rows whose tile does not fit 32-bit offsets, outputs whose tiles do not fit a launch: the kernels with 64-bit addresses."""
+    assert plan(5000, 1 << 23, 500) == plan(5000, 500, 500, x=1 << 23) == plan(5000, 500, 500, w=1 << 23) == MANY_32x32
+    assert plan((1 << 31) - 1, 16, 500) != TILE_256 and plan((1 << 31) - 1, 1, 511) == MANY_32x32
+    for n in (1, 1000, (1 << 31) - 1):
+        for d in (1, 1000, (1 << 31) - 1):
+            for o in (1, 1000, (1 << 31) - 1):
+                if n * d < 1 << 40 and n * o < 1 << 40 and d * o < 1 << 40:
+                    assert 0 <= plan(n, d, o) <= 7 and 0 <= plan(n, d, o, exact=True) <= 6
