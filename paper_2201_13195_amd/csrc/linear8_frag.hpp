@@ -30,13 +30,6 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ float e8m0_to_f32(uint32_t e) {
     return __uint_as_float(e == 255u ? 0x7FC00000u : e == 0u ? 0x00400000u : e << 23);
 }
-template <int SCALE>
-__device__ __forceinline__ float scale_at(const void *scales, int64_t at) {
-    if constexpr (SCALE == SCALE_F32)
-        return reinterpret_cast<const float *>(scales)[at];
-    else
-        return e8m0_to_f32(reinterpret_cast<const uint8_t *>(scales)[at]);
-}
 
 // The first `valid` bytes of 16, the others zero.
 __device__ __forceinline__ uint4 first_bytes(uint4 q, int64_t valid) {

@@ -32,20 +32,26 @@ __device__ __forceinline__ void for_each(F f) {
     for_each_of(std::make_integer_sequence<int, N>(), f);
 }
 
-// BT x BO outputs on NT x NO waves, STAGES steps of operands in LDS or on their way; PD fragments of W are read ahead, so that one
-// barrier a step stands PD fragments before its end; the loads of a step are spread over SPAN MFMAs behind it.
-template <int BT_, int BO_, int NT_, int NO_, int STAGES_, int SPAN_, int PER_SIMD_>
+// BT x BO outputs on NT x NO waves.  PD fragments of W are read ahead, so that the one barrier of a step stands PD fragments before
+// its end, and the loads of the step after the next, into the stage that is free then, have a whole step to arrive.  They are spread
+// over the MFMAs behind the barrier.  Measured beside it, bf16 results, in us:
+//   - a third stage for 128 x 128 tiles, of which a compute unit then holds one: 512 x 4096 -> 4096 with powers of two 26 -> 21, but
+//     512 x 1024 -> 4096 8.6 -> 8.7 and 1024 x 1024 -> 1024 7.9 -> 8.1
+//   - a second barrier, behind which half of a 256 x 256 tile's loads have half a step more: 16384 x 4096 -> 4096 with powers of two
+//     217 -> 212, with fp32 scales 228 -> 236
+//   - every other tile backwards along the contraction: 207 -> 209
+template <int BT_, int BO_, int NT_, int NO_>
 struct Tile8 {
-    static constexpr int BT = BT_, BO = BO_, NT = NT_, NO = NO_, STAGES = STAGES_, PD = 3, SPAN = SPAN_, PER_SIMD = PER_SIMD_;
+    static constexpr int BT = BT_, BO = BO_, NT = NT_, NO = NO_, PD = 3;
     static constexpr int WAVES = NT * NO, THREADS = 64 * WAVES;
     static constexpr int WT = BT / NT, WO = BO / NO, TJ = WT / 16, TU = WO / 16;  // of a wave: rows, 16-row tiles
     static constexpr int JX = BT / 8 / WAVES, JW = BO / 8 / WAVES, LOADS = JX + JW + 1;  // 1 KB loads of a wave and step, one of scales
     static constexpr int X_BYTES = BT * 128, W_BYTES = BO * 128, STAGE = X_BYTES + W_BYTES;
     static constexpr int XS_BYTES = BT * 4, SCALES = XS_BYTES + 256;  // of a stage: X's, W's
-    static constexpr int LDS_BYTES = STAGES * (STAGE + SCALES) + 256;  // (the last 256: of waves without a share of the scales)
+    static constexpr int LDS_BYTES = 2 * (STAGE + SCALES) + 256;  // (the last 256: of waves without a share of the scales)
     static constexpr int MFMAS = TU * TJ;
     static_assert(BT % (8 * WAVES) == 0 && BO % (8 * WAVES) == 0 && WT % 64 == 0 && WO % 64 == 0 && 128 % WO == 0, "shares of a wave");
-    static_assert(PD == 3 && TU % 4 == 0 && SPAN <= PD * TJ && STAGES >= 2 && LDS_BYTES <= 160 * 1024, "ring of four fragments, loads behind the barrier");
+    static_assert(PD == 3 && TU % 4 == 0 && LOADS <= PD * TJ && LDS_BYTES <= 160 * 1024, "ring of four fragments, loads behind the barrier");
 };
 
 // A wave-uniform value, which the compiler then keeps in a scalar register.
@@ -131,7 +137,7 @@ struct ScaleLoads8 {
 
 // CUT: the contraction is no multiple of 16.
 template <typename S, int F8, int SCALE, typename T, bool CUT>
-__global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(Linear8Args g) {
+__global__ void __launch_bounds__(S::THREADS, 2) linear8_tile_kernel(Linear8Args g) {
     constexpr bool EXACT = sizeof(T) == 4, IN_MFMA = SCALE == SCALE_E8M0 && !EXACT;
     constexpr int TJ = S::TJ, TU = S::TU, PD = S::PD, BT = S::BT, BO = S::BO;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[S::LDS_BYTES];
@@ -157,7 +163,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
     ScaleLoads8<S, SCALE> ls;
     lx.init(g.x.ld, g.d_in, lds0, wave, lane, [](int r) { return r / S::WT * S::WT + r % 16 * TJ + r % S::WT / 16; });
     lw.init(g.w.ld, g.d_in, lds0 + S::X_BYTES, wave, lane, [](int r) { return r / 32 * 32 + r % 16 / 4 * 8 + r / 16 % 2 * 4 + r % 4; });
-    ls.init(g, lds0 + S::STAGES * S::STAGE, lds0 + S::STAGES * (S::STAGE + S::SCALES), wave);
+    ls.init(g, lds0 + 2 * S::STAGE, lds0 + 2 * (S::STAGE + S::SCALES), wave);
     // The tile whose operands are requested after the one that is being requested.
     Span next_x, next_w;
     int64_t next_t0 = 0, next_o0 = 0;
@@ -171,14 +177,15 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
     };
     // The step that is being requested, and the stage it goes to.
     int asked = steps - 1;
-    uint32_t soff = 0, last = 0, into = S::STAGES - 1;
+    uint32_t soff = 0, last = 0, into = 1;
     auto begin = [&] {
         const bool turn = asked == steps - 1;
-        asked = turn ? 0 : asked + 1, into = into == S::STAGES - 1 ? 0 : into + 1;
+        asked = turn ? 0 : asked + 1, into ^= 1;
         lx.at.base = turn ? next_x.base : lx.at.base, lx.at.range = turn ? next_x.range : lx.at.range;
         lw.at.base = turn ? next_w.base : lw.at.base, lw.at.range = turn ? next_w.range : lw.at.range;
         ls.turn(turn);
-        soff = (uint32_t)asked * 128u, last = asked == steps - 1 ? 0xFFFFFFFFu : 0u;
+        // (a tile that is not there has no bytes, and no offset either: the check takes it from the range, unsigned)
+        soff = lx.at.range == 0 ? 0u : (uint32_t)asked * 128u, last = asked == steps - 1 ? 0xFFFFFFFFu : 0u;
     };
     auto load = [&](int i) {  // load i of that step: the scales first
         if (i == 0)
@@ -193,9 +200,8 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
     const uint32_t at0 = (uint32_t)(i16 * 128 + ((g4 ^ ((i16 >> 1) & 7)) << 4)), at1 = at0 ^ 64u;
     uint32_t from = 0, x0 = at0 + wt * S::WT * 128, x1 = at1 + wt * S::WT * 128, w0 = at0 + S::X_BYTES + wo * S::WO * 128, w1 = at1 + S::X_BYTES + wo * S::WO * 128;
     auto turn_stage = [&] {
-        const bool around = from == S::STAGES - 1;
-        const uint32_t by = around ? 0u - (uint32_t)((S::STAGES - 1) * S::STAGE) : (uint32_t)S::STAGE;
-        from = around ? 0 : from + 1, x0 += by, x1 += by, w0 += by, w1 += by;
+        const uint32_t by = from == 0 ? (uint32_t)S::STAGE : 0u - (uint32_t)S::STAGE;
+        from ^= 1, x0 += by, x1 += by, w0 += by, w1 += by;
     };
     auto fragment = [&](uint32_t a, uint32_t b, int tile) {
         union {
@@ -216,7 +222,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
     uint32_t w_byte = 0;  // address of the step's scale of W
     auto w_byte_of = [&](int64_t o0) { return (uint32_t)reinterpret_cast<uint64_t>(g.w.scales) + (uint32_t)((o0 + wo * S::WO) / kBlock8 * g.w.ld_scales); };
     auto read_scales = [&] {
-        const unsigned char *at = lds + S::STAGES * S::STAGE + from * S::SCALES;
+        const unsigned char *at = lds + 2 * S::STAGE + from * S::SCALES;
         ws_read = *reinterpret_cast<const uint32_t *>(at + S::XS_BYTES + wo * S::WO / kBlock8 * 4);
 #pragma unroll
         for (int q = 0; q < XS; ++q) xs_read[q] = *reinterpret_cast<const uint32_t *>(at + (wt * S::WT + i16 * TJ) * (SCALE == SCALE_F32 ? 4 : 1) + 4 * q);
@@ -247,8 +253,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
     constexpr int TAIL = PD * TJ;  // MFMAs behind the barrier
     constexpr int LOADS = S::LOADS;
     constexpr int STORES = TJ * TU / 2;  // of a wave, at least, where the tile has all its rows and columns
-    constexpr int AHEAD = (S::STAGES - 2) * LOADS;  // behind the loads of the next step
-    static_assert((S::STAGES - 1) * LOADS <= 63 && AHEAD + STORES <= 63, "what a wait can count");
+    static_assert(LOADS <= 63 && STORES <= 63, "what a wait can count");
     uint32_t position = blockIdx.x / 8;
     place(position);
     int64_t t0 = next_t0, o0 = next_o0;
@@ -256,13 +261,10 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) load(i);
     place(position + turns);
+    begin();
 #pragma unroll
-    for (int k = 1; k < S::STAGES; ++k) {
-        begin();
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) load(i);
-    }
-    wait_for_loads<(S::STAGES - 1) * LOADS>();
+    for (int i = 0; i < LOADS; ++i) load(i);
+    wait_for_loads<LOADS>();
     __syncthreads();
     read_first();
     read_scales();
@@ -297,12 +299,12 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
         }
         [[maybe_unused]] f32x4_t part[3];
         for_each<S::MFMAS + (IN_MFMA ? 0 : 2)>([&](auto index) __attribute__((always_inline)) {
-            constexpr int i = decltype(index)::value, u = i / TJ, j = i % TJ, q = i - (TU - PD) * TJ, slot = q >= 0 ? q : i + TAIL;
+            constexpr int i = decltype(index)::value, u = i / TJ, j = i % TJ, q = i - (TU - PD) * TJ;
             if constexpr (q == 0) {  // every fragment of W of this stage is in registers, the next step's data are there
-                if (stored && left > steps - (S::STAGES - 1))
-                    wait_for_loads<AHEAD + STORES>();  // (behind those loads the results of the tile before went out)
+                if (stored && left == steps)
+                    wait_for_loads<STORES>();  // (behind the loads the results of the tile before went out)
                 else
-                    wait_for_loads<AHEAD>();
+                    wait_for_loads<0>();
                 __syncthreads();
                 begin();
                 turn_stage();
@@ -324,7 +326,7 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
                 if constexpr (q == 1) read_scales();
                 if constexpr (u == TU - 1) xf[j] = fragment(x0, x1, j);
                 for_each<LOADS>([&](auto l) __attribute__((always_inline)) {
-                    if constexpr (decltype(l)::value * S::SPAN / LOADS == slot) load(decltype(l)::value);
+                    if constexpr (decltype(l)::value * TAIL / LOADS == q) load(decltype(l)::value);
                 });
             }
             if constexpr (!IN_MFMA && i >= 2) {
@@ -379,14 +381,14 @@ __global__ void __launch_bounds__(S::THREADS, S::PER_SIMD) linear8_tile_kernel(L
     wait_for_loads<0>();  // (of no tile: zeros, but into LDS that is another work-group's from here on)
 }
 
-typedef Tile8<256, 256, 4, 2, 2, 12, 2> Large8;   // 8 waves of 64 x 128
-typedef Tile8<128, 128, 2, 2, 2, 12, 2> Mid8;     // 4 waves of 64 x 64, two work-groups to a compute unit
+typedef Tile8<256, 256, 4, 2> Large8;   // 8 waves of 64 x 128
+typedef Tile8<128, 128, 2, 2> Mid8;     // 4 waves of 64 x 64, two work-groups to a compute unit
 
 template <typename S, int F8, int SCALE, typename T>
 void launch_tile(const Linear8Args &g, hipStream_t stream) {
     const int64_t tiles = (g.n + S::BT - 1) / S::BT * ((g.d_out + S::BO - 1) / S::BO), places = 256 * (160 * 1024 / S::LDS_BYTES);
     const int64_t steps = (g.d_in + kBlock8 - 1) / kBlock8;
-    const unsigned grid = (unsigned)(steps >= S::STAGES && tiles > places ? places : tiles);  // (requests reach into one further tile, no more)
+    const unsigned grid = (unsigned)(steps >= 2 && tiles > places ? places : tiles);  // (requests reach into one further tile, no more)
     if (g.d_in % 16 != 0)
         linear8_tile_kernel<S, F8, SCALE, T, true><<<grid, S::THREADS, 0, stream>>>(g);
     else
