@@ -6,7 +6,7 @@ import subprocess
 import pytest
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2201_13195_amd", "csrc")
-FEW_16x16, FEW_16x32, FEW_32x32, FEW_64x32, MANY_16x64, MANY_32x32, TILE_128, TILE_256 = range(8)
+FEW_16x16, FEW_16x32, FEW_32x32, FEW_64x32, MANY_16x64, MANY_32x32, TILE_64x128, TILE_128_SPLIT, TILE_128, TILE_256 = range(10)
 UNITS = 256
 
 # (n, d_in, d_out) of each kernel, bf16 and fp32 results; tests/test_gpu_linear8.py runs them.
@@ -17,7 +17,11 @@ KERNELS = [
     ((333, 1000, 1111), FEW_64x32, FEW_64x32), ((128, 2048, 4000), FEW_64x32, FEW_64x32),
     ((1, 520, 9001), MANY_16x64, MANY_16x64), ((16, 136, 20000), MANY_16x64, MANY_16x64),
     ((20, 520, 9001), MANY_32x32, MANY_32x32), ((32, 131, 17000), MANY_32x32, MANY_32x32),
-    ((600, 400, 1200), TILE_128, TILE_128), ((1100, 2050, 1030), TILE_128, TILE_128),
+    ((600, 400, 1200), TILE_128, TILE_64x128), ((1100, 2050, 1030), TILE_64x128, TILE_64x128),
+    ((500, 777, 3000), TILE_64x128, TILE_64x128),     # seven blocks: the second group has none in the last step
+    ((260, 1160, 4090), TILE_64x128, TILE_64x128), ((100, 1111, 9000), TILE_64x128, TILE_64x128),
+    ((900, 2600, 4000), TILE_128_SPLIT, TILE_128_SPLIT), ((2000, 2440, 2040), TILE_128_SPLIT, TILE_128_SPLIT),
+    ((1500, 2513, 2500), TILE_128_SPLIT, TILE_128_SPLIT), ((700, 600, 4000), TILE_128, TILE_128),
     ((2100, 250, 4100), TILE_128, TILE_128),          # more tiles than places, two steps: a work-group has a second tile
     ((2100, 128, 4100), TILE_128, TILE_128),          # one step
     ((4096, 1024, 4096), TILE_256, TILE_128), ((4300, 1000, 4090), TILE_256, TILE_128),      # (the second: two rounds of tiles)
@@ -49,7 +53,7 @@ def test_kernels_by_shape(plan, shape, bf16, f32):
 
 
 def test_every_kernel_is_among_them():
-    assert {k for _, k, _ in KERNELS} == set(range(8))
+    assert {k for _, k, _ in KERNELS} == set(range(10))
 
 
 def test_few_outputs_never_take_more_than_a_round(plan):
@@ -65,10 +69,23 @@ def test_few_outputs_never_take_more_than_a_round(plan):
                 assert (k == MANY_16x64) == (n <= 16) and (k == MANY_32x32) == (16 < n <= 32)
 
 
+def test_groups_that_share_the_contraction_have_a_compute_unit_each(plan):
+    for n in (33, 100, 333, 512, 1000, 1024, 2048, 4096):
+        for d_out in (100, 1024, 2048, 3000, 4096, 9000, 20000):
+            for d_in in (64, 400, 768, 1024, 2500, 4096):
+                for exact in (False, True):
+                    k = plan(n, d_in, d_out, exact)
+                    if k < TILE_64x128:
+                        continue
+                    half, whole, steps = groups(n, d_out, 64, 128), groups(n, d_out, 128, 128), -(-d_in // 128)
+                    assert (k == TILE_64x128) == (half <= UNITS and steps >= (3 if exact else 6))
+                    assert (k == TILE_128_SPLIT) == (k != TILE_64x128 and whole <= UNITS and steps >= 20)
+
+
 def test_large_ones_take_the_large_tile(plan):
     assert plan(16384, 4096, 4096) == plan(16384, 1024, 4096) == plan(16384, 4096, 1024) == TILE_256
     assert plan(8192, 1024, 1024) == plan(4096, 768, 768) == plan(2048, 2048, 2048) == TILE_128
-    assert all(plan(n, d, d, exact=True) == TILE_128 for n in (2000, 20000) for d in (1000, 4096))
+    assert all(plan(20000, d, d, exact=True) == TILE_128 for d in (1000, 4096)) and plan(2100, 1000, 1000, exact=True) == TILE_128
 
 
 def test_operands_beyond_32_bits_of_a_tile(plan):
@@ -79,4 +96,4 @@ def test_operands_beyond_32_bits_of_a_tile(plan):
         for d in (1, 1000, (1 << 31) - 1):
             for o in (1, 1000, (1 << 31) - 1):
                 if n * d < 1 << 40 and n * o < 1 << 40 and d * o < 1 << 40:
-                    assert 0 <= plan(n, d, o) <= 7 and 0 <= plan(n, d, o, exact=True) <= 6
+                    assert 0 <= plan(n, d, o) < 10 and 0 <= plan(n, d, o, exact=True) < TILE_256
