@@ -134,6 +134,7 @@ class RMMNormFunction(torch.autograd.Function):
         return None if r.Y is None else r.Y.reshape(X.shape), None if residual is None else H, r.Y8, r.scales
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dY, dH, _, __):
         H, weight, rstd = ctx.saved_tensors
         dX, dweight = dH, None
@@ -185,6 +186,7 @@ class RMMLinear8Function(torch.autograd.Function):
         return Y.reshape(*X.shape[:-1], W.shape[0])
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dY):
         W, X_proj = ctx.saved_tensors
         scale_dtype, grad_f8 = ctx.formats
@@ -205,7 +207,8 @@ class RMMLinear8(RMMLinear):
     Rows8 of an RMMNorm in front of it.  `scale_dtype`: torch.float32, or torch.float8_e8m0fnu for powers of two;
     `grad_f8`: the format of dY's rows.
 
-    pack() keeps W's 8-bit form for calls without gradients, until W changes."""
+    pack() keeps W's 8-bit form for calls without gradients, until W changes: such a call refuses then (a change through
+    weight.data, which torch does not count, goes unnoticed)."""
 
     def __init__(self, in_features, out_features, bias=True, rho=0.1, k=None, kind=binding.GAUSSIAN, seed=0, layer_id=None,
                  device="cuda", dtype=torch.bfloat16, scale_dtype=torch.float8_e8m0fnu, grad_f8=torch.float8_e4m3fn):
@@ -234,6 +237,9 @@ class RMMLinear8(RMMLinear):
         rows = X if isinstance(X, Rows8) else None
         if rows is not None and rows.data.shape[1] != self.in_features:
             raise ValueError("RMMLinear8: rows of %d columns, in_features is %d" % (rows.data.shape[1], self.in_features))
+        full = X if rows is None else rows.Y
+        if full is not None and full.dtype != self.weight.dtype:
+            raise TypeError("RMMLinear8: X must have the weight's dtype, %s, has %s" % (self.weight.dtype, full.dtype))
         if not torch.is_grad_enabled():
             if rows is None:
                 lead = X.shape[:-1]

@@ -105,3 +105,14 @@ def test_layers_refuse_unknown_formats():
         rmm.RMMLinear8(8, 8, device="cpu", grad_f8=torch.float16)
     with pytest.raises(TypeError):
         rmm.RMMLinear8(8, 8, device="cpu", scale_dtype=torch.float16)
+
+
+def test_the_layer_refuses_another_dtype_than_its_weights():
+    layer = rmm.RMMLinear8(32, 8, device="cpu")
+    X = torch.zeros(4, 32)
+    rows = rmm.Rows8(X, X.to(torch.float8_e4m3fn), torch.zeros(1, 4), (4,))
+    for x in (X, rows):
+        with pytest.raises(TypeError, match="the weight's dtype"):
+            layer(x)
+        with torch.no_grad(), pytest.raises(TypeError, match="the weight's dtype"):
+            layer(x)

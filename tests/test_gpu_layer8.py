@@ -222,3 +222,24 @@ def test_two_streams_at_once():
                 got.append(chain())
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for out in got for a, b in zip(out, want))
+
+
+def test_gradients_of_gradients_are_refused():
+    norm, layer = rmm.RMMNorm(64), rmm.RMMLinear8(64, 32)
+    for f in (norm, layer):
+        X = torch.randn(8, 64, device=DEV, dtype=torch.bfloat16, requires_grad=True)
+        g, = torch.autograd.grad(f(X).float().square().sum(), X, create_graph=True)
+        with pytest.raises(RuntimeError, match="differentiate twice"):
+            g.float().sum().backward()
+
+
+def test_packed_weights_that_changed_are_refused():
+    layer = rmm.RMMLinear8(64, 32)
+    X = torch.randn(8, 64, device=DEV, dtype=torch.bfloat16)
+    with torch.no_grad():
+        want = layer(X)
+        assert torch.equal(layer.pack()(X), want)
+        layer.weight.mul_(2)
+        with pytest.raises(RuntimeError, match="has changed"):
+            layer(X)
+        assert torch.equal(layer.pack()(X), 2 * want)
