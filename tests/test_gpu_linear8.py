@@ -182,3 +182,56 @@ def test_large_offsets():
     Y = rmm.rmm_linear8(*x, w8.view(E4), ws)
     first = rmm.rmm_linear8(*x, *w)
     assert torch.equal(Y[-300:, :128], first[-300:]) and torch.equal(Y[-300:, 128 * 200:128 * 201], first[-300:])
+
+
+TILES = [(2100, 999, 520), (300, 1000, 3001), (3000, 2501, 1000), (2100, 300, 1500), (4300, 1001, 4090)]     # 64 x 128 twice, 128 split, 128, 256
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("scale_dtype", eight.SCALES)
+@pytest.mark.parametrize("n,d_in,d_out", TILES)
+def test_tiles_take_nothing_from_behind_their_operands(n, d_in, d_out, scale_dtype, dtype):
+    """NaN behind columns, rows and scales of both operands, and around a Y that is given: the same bits, and nothing else written."""
+    x, w, _ = operands(n, d_in, d_out, E4, scale_dtype)
+    want = rmm.rmm_linear8(*x, *w, dtype=dtype)
+    raw = torch.float32 if scale_dtype == torch.float32 else torch.uint8
+    data, scales = [], []
+    for t, s, high, wide in ((x[0], x[1], 0, 80), (w[0], w[1], 1, 3)):
+        b = torch.full((t.shape[0] + 256, (d_in + 15) // 16 * 16 + 160), 0x7F, dtype=torch.uint8, device=DEV)
+        b[:t.shape[0], :d_in] = t.view(torch.uint8)
+        data.append(b.view(E4)[:t.shape[0], :d_in])
+        pitch = (s.shape[1] + wide + 15) // 16 * 16
+        c = torch.full((s.shape[0] + high + 1, pitch), float("nan"), device=DEV).to(scale_dtype)
+        c.view(raw)[:s.shape[0], :s.shape[1]] = s.view(raw)
+        scales.append(c[:s.shape[0], :s.shape[1]])
+    around = torch.full(((n + 300) * d_out,), 7.0, dtype=dtype, device=DEV)
+    Y = around[:n * d_out].view(n, d_out)
+    rmm.rmm_linear8(data[0], scales[0], data[1], scales[1], dtype=dtype, Y=Y)
+    assert torch.equal(Y, want) and bool((around[n * d_out:] == 7.0).all())
+    assert torch.equal(rmm.rmm_linear8(*x, *w, dtype=dtype), want)
+
+
+@pytest.mark.parametrize("scale_dtype", eight.SCALES)
+@pytest.mark.parametrize("n,d_in,d_out", TILES)
+def test_no_numbers_in_one_block_of_a_tile(n, d_in, d_out, scale_dtype):
+    """A token with an infinity in each block in turn, and no others, is NaN."""
+    x, w, _ = operands(n, d_in, d_out, E4, scale_dtype)
+    want = rmm.rmm_linear8(*x, *w)
+    blocks = (d_in + 127) // 128
+    tokens = torch.arange(blocks) * (n // blocks)
+    X = torch.zeros(n, d_in)
+    X[tokens, torch.arange(blocks) * 128 + 5] = float("inf")
+    bad = rmm.rmm_quantize8(X.to(DEV), scale_dtype=scale_dtype)
+    data, scales = x[0].clone(), x[1].clone()
+    raw = torch.float32 if scale_dtype == torch.float32 else torch.uint8
+    for b, t in enumerate(tokens.tolist()):
+        data.view(torch.uint8)[t, 128 * b:128 * b + 128] = bad[0].view(torch.uint8)[t, 128 * b:128 * b + 128]
+        scales.view(raw)[b, t] = bad[1].view(raw)[b, t]
+    wide = rmm.rmm_quantize8(torch.zeros(n, d_in, device=DEV), scale_dtype=scale_dtype)
+    wide[0].view(torch.uint8).copy_(data.view(torch.uint8))
+    wide[1].view(raw).copy_(scales.view(raw))
+    Y = rmm.rmm_linear8(*wide, *w)
+    assert bool(Y[tokens.to(DEV)].isnan().all())
+    others = torch.ones(n, dtype=torch.bool, device=DEV)
+    others[tokens.to(DEV)] = False
+    assert torch.equal(Y[others], want[others])
