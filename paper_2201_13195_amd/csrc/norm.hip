@@ -67,9 +67,11 @@ __device__ __forceinline__ Rstd rstd_of(double sum, const NormArgs &g) {
 }
 
 // Eight columns of y = h rstd w to 8 bits.  An 8-bit number is decided by where y / s lies between two of the format's, and
-// is as far off as they are apart where y is off by little and crosses over: y is made to twice the bits of fp32 here, as y + low.
+// is as far off as they are apart where y is off by little and crosses over: y is made to twice the bits of fp32 here, as y + low, and
+// so is the largest magnitude, whose quotient is then rounded once.
 template <int F8, int SCALE>
 __device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col, int lane, const float (&h)[8], const Rstd &r, const float (&w)[8]) {
+#pragma clang fp contract(off)  // (what a rounding left out would be counted twice where a sum takes the product whole)
     float y[8], low[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -77,7 +79,13 @@ __device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col
         const float v = p * w[i], v_low = fmaf(p_low, w[i], fmaf(p, w[i], -v));
         y[i] = v + v_low, low[i] = v_low - (y[i] - v);
     }
-    const BlockScale s = block_scale<F8, SCALE>(max_of_16(amax8(y)));
+    const uint32_t most = max_of_16(amax8(y));
+    float more = -INFINITY;  // of those as large in fp32, what is missing of the largest
+#pragma unroll
+    for (int i = 0; i < 8; ++i) more = magnitude(y[i]) == most ? fmaxf(more, y[i] < 0.0f ? -low[i] : low[i]) : more;
+    more = max_of_16(more);
+    const float amax = __uint_as_float(most), q = amax / top_of<F8>();
+    const BlockScale s = block_scale<F8, SCALE>(fmaf(fmaf(-q, top_of<F8>(), amax) + more, 1.0f / top_of<F8>(), q));
     if (col < g.d) {
         store8_bytes(g.y8.data + row * g.y8.ld + col, g.d - col, to_f8<F8, SCALE>(y, low, s));
         if ((lane & 15) == 0) store_scale<SCALE>(g.y8.scales, col / kBlock8 * g.y8.ld_scales + row, s);
@@ -125,14 +133,15 @@ __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_kernel(NormArgs 
         if (g.residual != nullptr)
 #pragma unroll
             for (int c = 0; c < CH; ++c) r[c] = load_run<T, MODE>((const T *)g.residual + row * g.d, p.col(c), g.d);
-        float h[CH][8], sum = 0.0f;
+        float h[CH][8];
+        double sum = 0.0;  // (memory bounds the kernel all the same; in fp32 y would not have the bits that put8 makes it to)
 #pragma unroll
         for (int c = 0; c < CH; ++c) make_h<T, MODE>(g, row, p.col(c), x[c], r[c], h[c]);
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(h[c][i], h[c][i], sum);
-        const Rstd rstd = rstd_of(row_sum<WPR>((double)sum, red, turn), g);
+            for (int i = 0; i < 8; ++i) sum = fma((double)h[c][i], (double)h[c][i], sum);
+        const Rstd rstd = rstd_of(row_sum<WPR>(sum, red, turn), g);
         if (g.rstd != nullptr && p.part == 0 && p.lane == 0) g.rstd[row] = rstd.high;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
@@ -163,13 +172,14 @@ __global__ void __launch_bounds__(1024) rms_norm_long_kernel(NormArgs g) {
     const Place<16> p;
     int turn = 0;
     for (int64_t row = blockIdx.x; row < g.n; row += gridDim.x, ++turn) {
-        float h[8], sum = 0.0f;
+        float h[8];
+        double sum = 0.0;
         for (int c = 0; p.col(c) < g.d; ++c) {
             take_h<T>(g, row, p.col(c), h);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(h[i], h[i], sum);
+            for (int i = 0; i < 8; ++i) sum = fma((double)h[i], (double)h[i], sum);
         }
-        const Rstd rstd = rstd_of(row_sum<16>((double)sum, red, turn), g);
+        const Rstd rstd = rstd_of(row_sum<16>(sum, red, turn), g);
         if (g.rstd != nullptr && threadIdx.x == 0) g.rstd[row] = rstd.high;
         NormArgs again = g;  // (what was written is read back, by the thread that wrote it; the buffer may be that of X)
         if (g.residual != nullptr && g.H != nullptr) again.X = g.H, again.residual = nullptr;

@@ -191,10 +191,11 @@ struct BlockScale {
     uint32_t stored;
     bool slow;
 };
+template <int F8>
+__device__ __forceinline__ constexpr float top_of() { return F8 == F8_E4M3 ? 448.0f : 57344.0f; }
+// (`q`: amax / top)
 template <int F8, int SCALE>
-__device__ __forceinline__ BlockScale block_scale(uint32_t amax_bits) {
-    constexpr float TOP = F8 == F8_E4M3 ? 448.0f : 57344.0f;
-    const float q = __uint_as_float(amax_bits) / TOP;
+__device__ __forceinline__ BlockScale block_scale(float q) {
     const float s = q < 0x1p-126f ? 0x1p-126f : q;  // (NaN stays)
     BlockScale b;
     if constexpr (SCALE == SCALE_F32) {
@@ -208,6 +209,11 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t amax_bits) {
     // (then the remainder below would not be exact, or s is no number)
     b.slow = !(b.s > 0x1p-90f && b.s < 0x1p125f);
     return b;
+}
+
+template <int F8, int SCALE>
+__device__ __forceinline__ BlockScale block_scale(uint32_t amax_bits) {
+    return block_scale<F8, SCALE>(__uint_as_float(amax_bits) / top_of<F8>());
 }
 
 // v / s, correctly rounded.  A power of two: the product with its inverse is exact.  Else from q = v inv, which is a unit
@@ -280,6 +286,12 @@ __device__ __forceinline__ uint32_t max_of_16(uint32_t m) {
     m = max(m, from_lane<LANE_XOR1>(m)), m = max(m, from_lane<LANE_XOR2>(m));
     m = max(m, from_lane<LANE_MIRROR8>(m));
     return max(m, from_lane<LANE_MIRROR16>(m));
+}
+__device__ __forceinline__ float max_of_16(float v) {
+    auto with = [&](uint32_t other) { v = fmaxf(v, __uint_as_float(other)); };
+    with(from_lane<LANE_XOR1>(__float_as_uint(v))), with(from_lane<LANE_XOR2>(__float_as_uint(v)));
+    with(from_lane<LANE_MIRROR8>(__float_as_uint(v))), with(from_lane<LANE_MIRROR16>(__float_as_uint(v)));
+    return v;
 }
 template <int CTRL>
 __device__ __forceinline__ float plus_lane(float v) {

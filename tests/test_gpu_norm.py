@@ -79,6 +79,25 @@ def test_rows_in_8_bits(n, d, f8, scale_dtype):
         assert only.Y is None and torch.equal(eight.bytes_of(only.Y8), eight.bytes_of(r.Y8))
 
 
+@pytest.mark.parametrize("scale_dtype", eight.SCALES)
+@pytest.mark.parametrize("f8", eight.F8)
+@pytest.mark.parametrize("n,d,residual", [(700, 1001, False), (500, 768, True), (300, 2500, True), (90, 6001, False), (20, 40000, True)])
+def test_8_bit_rows_are_those_of_the_result_in_64_bits(n, d, residual, f8, scale_dtype):
+    """Every scale and byte: Y is made to about 2^-46, and of some 2^20 quotients none lies that near to a number half way between two."""
+    for dtype in DTYPES:
+        t = inputs(n, d, dtype, residual, seed=5)
+        _, _, y = forward64(t["X"], t["weight"], t["residual"], dtype)
+        r = rmm.rmm_rms_norm(t["X"], t["weight"], t["residual"], EPS, need_Y=False, f8=f8, scale_dtype=scale_dtype)
+        y = torch.nn.functional.pad(y.cpu(), (0, eight.blocks(d) * 128 - d)).view(n, -1, 128)
+        s = (y.abs().amax(2) / eight.TOP[f8]).clamp(min=2.0 ** -126).float()
+        if scale_dtype == torch.float8_e8m0fnu:
+            m, e = torch.frexp(s)
+            s = torch.ldexp(torch.ones_like(s), torch.where(m == 0.5, e - 1, e))
+        assert torch.equal(eight.scale64(r.scales), s.t().double())
+        want = (y / s[..., None].double()).float().to(f8).view(n, -1)[:, :d]
+        assert torch.equal(eight.bytes_of(r.Y8), eight.bytes_of(want))
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("n,d", SHAPES + [(600, 768), (2100, 256), (1030, 4096), (513, 1001)])
 def test_backward(n, d, dtype):
