@@ -68,7 +68,8 @@ __device__ __forceinline__ Rstd rstd_of(double sum, const NormArgs &g) {
 
 // Eight columns of y = h rstd w to 8 bits.  An 8-bit number is decided by where y / s lies between two of the format's, and
 // is as far off as they are apart where y is off by little and crosses over: y is made to twice the bits of fp32 here, as y + low, and
-// so is the largest magnitude, whose quotient is then rounded once.
+// so is the largest magnitude, whose quotient is then rounded once.  A power of two takes y alone: its quotients are exact, and which
+// power it is does not hang on the last bits.
 template <int F8, int SCALE>
 __device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col, int lane, const float (&h)[8], const Rstd &r, const float (&w)[8]) {
 #pragma clang fp contract(off)  // (what a rounding left out would be counted twice where a sum takes the product whole)
@@ -80,12 +81,15 @@ __device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col
         y[i] = v + v_low, low[i] = v_low - (y[i] - v);
     }
     const uint32_t most = max_of_16(amax8(y));
-    float more = -INFINITY;  // of those as large in fp32, what is missing of the largest
+    const float amax = __uint_as_float(most);
+    float q = amax / top_of<F8>();
+    if constexpr (SCALE == SCALE_F32) {
+        float more = -INFINITY;  // of those as large in fp32, what is missing of the largest
 #pragma unroll
-    for (int i = 0; i < 8; ++i) more = magnitude(y[i]) == most ? fmaxf(more, y[i] < 0.0f ? -low[i] : low[i]) : more;
-    more = max_of_16(more);
-    const float amax = __uint_as_float(most), q = amax / top_of<F8>();
-    const BlockScale s = block_scale<F8, SCALE>(fmaf(fmaf(-q, top_of<F8>(), amax) + more, 1.0f / top_of<F8>(), q));
+        for (int i = 0; i < 8; ++i) more = magnitude(y[i]) == most ? fmaxf(more, y[i] < 0.0f ? -low[i] : low[i]) : more;
+        q = fmaf(fmaf(-q, top_of<F8>(), amax) + max_of_16(more), 1.0f / top_of<F8>(), q);
+    }
+    const BlockScale s = block_scale<F8, SCALE>(q);
     if (col < g.d) {
         store8_bytes(g.y8.data + row * g.y8.ld + col, g.d - col, to_f8<F8, SCALE>(y, low, s));
         if ((lane & 15) == 0) store_scale<SCALE>(g.y8.scales, col / kBlock8 * g.y8.ld_scales + row, s);
