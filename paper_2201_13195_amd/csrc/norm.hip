@@ -393,7 +393,9 @@ __global__ void __launch_bounds__(1024) sum_parts_kernel(const float *__restrict
 constexpr int64_t columns(int ch, int wpr) { return (int64_t)ch * wpr * 64 * kRun; }
 int64_t rows_a_group(int64_t d) { return d <= columns(2, 1) ? 4 : 1; }
 constexpr int64_t kMostForward = 2048, kMostBackward = 512;  // work-groups: eight, two for each compute unit
-bool long_rows(int64_t d) { return d > columns(2, 16); }  // of the backward pass
+// (four runs a lane in 16 waves are more than their registers hold: with 8-bit rows, 1000 x 32768 bf16 85 us, read twice 62; 2048 x 16384
+// with four runs 134, with two 58)
+bool long_rows(int64_t d) { return d > columns(2, 16); }
 int64_t backward_groups(int64_t n, int64_t d) {
     if (long_rows(d)) return n < 16 ? n : 16;
     const int64_t groups = (n + rows_a_group(d) - 1) / rows_a_group(d);
@@ -426,8 +428,8 @@ hipError_t launch_rms_norm(const T *X, const T *residual, const T *weight, T *H,
         LAUNCH(rms_norm_kernel, 2, 4, 256);
     else if (d <= columns(4, 4))
         LAUNCH(rms_norm_kernel, 4, 4, 256);
-    else if (d <= columns(4, 16))
-        LAUNCH(rms_norm_kernel, 4, 16, 1024);
+    else if (!long_rows(d))
+        LAUNCH(rms_norm_kernel, 2, 16, 1024);
     else
         rms_norm_long_kernel<T><<<grid, 1024, 0, stream>>>(g);
     return hipGetLastError();
