@@ -211,8 +211,8 @@ struct NormBackwardArgs {
     int64_t n, d;
 };
 
-// What is read of a row; with up to four waves a row, that of the next row is requested before this one is reduced (16 waves are 128
-// registers each, and enough requests between them).
+// What is read of a row; that of the next row is requested before this one is reduced (not with two runs a lane in 16 waves, 128
+// registers each: there are enough requests between them).  4096 x 8192 bf16: one run a lane 57 us, two, half of the lanes idle, 73.
 template <typename T, int CH>
 struct BackwardRow {
     Run8<T> dy[CH], h[CH], dh[CH];
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_backward_kernel(
     }
     const int64_t step = (int64_t)gridDim.x * p.ROWS;
     int64_t row = (int64_t)blockIdx.x * p.ROWS + p.row;
-    constexpr bool AHEAD = WPR < 16;
+    constexpr bool AHEAD = WPR < 16 || CH == 1;
     BackwardRow<T, CH> now, next;
     if (AHEAD && row < g.n) load_row<T, CH, WPR, MODE>(now, g, p, row);
     for (int turn = 0; row < g.n; row += step, ++turn) {
@@ -455,6 +455,8 @@ hipError_t launch_rms_norm_backward(const T *dY, const T *dH, const T *H, const 
         LAUNCH(rms_norm_backward_kernel, 1, 4, 256);
     } else if (d <= columns(2, 4)) {
         LAUNCH(rms_norm_backward_kernel, 2, 4, 256);
+    } else if (d <= columns(1, 16)) {
+        LAUNCH(rms_norm_backward_kernel, 1, 16, 1024);
     } else {
         LAUNCH(rms_norm_backward_kernel, 2, 16, 1024);
     }
