@@ -235,3 +235,40 @@ def test_no_numbers_in_one_block_of_a_tile(n, d_in, d_out, scale_dtype):
     others = torch.ones(n, dtype=torch.bool, device=DEV)
     others[tokens.to(DEV)] = False
     assert torch.equal(Y[others], want[others])
+
+
+def test_every_tile_kernel_in_a_graph_replayed():
+    """All in one capture, on inputs that change between the replays; two of them side by side on streams of their own."""
+    ops = [operands(*shape, E4, eight.SCALES[i % 2]) for i, shape in enumerate(TILES)]
+    out = [torch.empty(x[0].shape[0], w[0].shape[0], dtype=torch.bfloat16, device=DEV) for x, w, _ in ops]
+
+    def run():
+        for (x, w, _), y in zip(ops, out):
+            rmm.rmm_linear8(*x, *w, Y=y)
+
+    side, beside = torch.cuda.Stream(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for step in range(3):
+        for x, _, _ in ops:
+            raw = x[0].view(torch.uint8)
+            raw.copy_(raw.roll(1 + step, 0))
+        want = [rmm.rmm_linear8(*x, *w) for x, w, _ in ops]
+        for y in out:
+            y.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        beside.wait_stream(torch.cuda.current_stream())
+        again = [torch.empty_like(y) for y in out]
+        with torch.cuda.stream(beside):
+            for (x, w, _), y in zip(ops, again):
+                rmm.rmm_linear8(*x, *w, Y=y)
+        run_here = [rmm.rmm_linear8(*x, *w) for x, w, _ in ops]
+        torch.cuda.synchronize()
+        for a, b, c, d in zip(want, out, again, run_here):
+            assert torch.equal(a, b) and torch.equal(a, c) and torch.equal(a, d)
