@@ -13,25 +13,30 @@ enum {
     LINEAR8_FEW_64x32 = 3,
     LINEAR8_MANY_16x64 = 4,
     LINEAR8_MANY_32x32 = 5,
-    LINEAR8_TILE_64x128 = 6,
-    LINEAR8_TILE_128_SPLIT = 7,
-    LINEAR8_TILE_128 = 8,
-    LINEAR8_TILE_256 = 9
+    LINEAR8_MANY_64x32 = 6,
+    LINEAR8_TILE_64x128 = 7,
+    LINEAR8_TILE_128_SPLIT = 8,
+    LINEAR8_TILE_128 = 9,
+    LINEAR8_TILE_256 = 10
 };
 
 // A row per rule, times in us of bf16 results measured on both sides of it (256 compute units):
 //   - the smallest FEW kernel with no more work-groups than compute units: its time is one round of a latency and the contraction.
-//       24 x 4096 -> 1024 16x16 6.2, 16x32 7.9, 128 x 128 tiles 20;   128 x 768 -> 768 16x16 4.0 (384 work-groups), 16x32 3.6, 32x32 4.2;
-//       64 x 4096 -> 4096 16x32 13.7 (512), 32x32 10.5, 64x32 14.8;   333 x 1000 -> 1111 32x32 7.0 (385), 64x32 5.7, 128 x 128 tiles 10.5
-//   - up to 32 tokens and more outputs than that: the weights are read once, whatever the tile, and four waves of more outputs keep more of
-//     them in flight.  1 x 4096 -> 32000 (131 MB) 16x16 32.9, MANY 16x64 21.9, 128 x 128 tiles 27.5;  32 x 4096 -> 16384 MANY 32x32 18.6,
-//     128 x 128 tiles 26.4.  33 tokens and more would read them twice: 33 x 1024 -> 16384 MANY 32x32 9.7, 128 x 128 tiles 8.3
+//       24 x 4096 -> 1024 16x16 4.3, 16x32 4.5, 128 x 128 tiles 20;   128 x 768 -> 768 16x16 3.9 (384 work-groups), 16x32 3.4, 32x32 3.8;
+//       64 x 4096 -> 4096 16x32 8.7 (512), 32x32 7.0, 64x32 7.5;   128 x 4096 -> 4096 32x32 10.1 (512), 64x32 8.0, MANY 32x32 8.8
+//   - instead of 64x32 MANY 32x32, two work-groups to a compute unit, where its four waves have no more than two blocks each:
+//       333 x 1000 -> 1111 4.8 (64x32 5.1);   fp32 results 5.1 (5.5)
+//   - up to 64 tokens and more outputs than that: the weights are read once, whatever the tile, and four waves of more outputs keep more of
+//     them in flight.  1 x 4096 -> 32000 (131 MB) 16x32 23.9, MANY 16x64 20.2, 128 x 128 tiles 27.9;  32 x 4096 -> 16384 MANY 32x32 12.8,
+//     64x32 13.5, 64 x 128 tiles 15.1;  48 x 4096 -> 16384 MANY 32x32 20.8, 64x32 14.1, 64 x 128 tiles 15.6
+//   - MANY 64x32 for up to two work-groups a compute unit too:  1024 x 1024 -> 1024 5.8 (64 x 128 tiles 7.1);  256 x 4096 -> 4096 11.8 (14.5),
+//     but 400 x 768 -> 3000 (658) 8.1 (7.1) and 512 x 4096 -> 4096 (1024) 22.5 (15.2)
 //   - tiles otherwise, up to a compute unit's one by two groups of waves that share the contraction, where it is long enough:
 //     64 x 128 from six blocks of it on (three for fp32 results, whose every block is four times the work), 128 x 128 from twenty.
-//       512 x 4096 -> 4096 64 x 128 16.9, 128 x 128 split 22.0, as below 26.6;   1024 x 1024 -> 1024 7.5, 8.8, 8.1;   512 x 640 -> 4096 7.3, 8.5, 7.1;
+//       512 x 4096 -> 4096 64 x 128 16.9, 128 x 128 split 22.0, as below 26.6;   512 x 1024 -> 4096 8.1, 9.3, 8.6;   512 x 640 -> 4096 7.3, 8.5, 7.1;
 //       1024 x 4096 -> 4096 (512 of 64 x 128) 31.4, 25.1, 28.9;   1024 x 2560 -> 4096 22.9, 17.3, 18.3;   1024 x 2048 -> 4096 20.1, 14.6, 14.6
-//   - as many as there are, one group of waves each.  A 256 x 256 tile is 1.2 us a step of 128 and 3 us of its own, with a compute unit to itself; two 128 x 128 tiles
-//     share one, 0.95 us a step of both and 2 us:  8192 x 1024 -> 1024 256 18.8, 128 14.5;  4096 x 1024 -> 4096 256 21.8, 128 24.5;
+//   - as many as there are, one group of waves each.  A 256 x 256 tile is 1.2 us a step of 128 and 3 us of its own, with a compute unit
+//     to itself; two 128 x 128 tiles share one, 0.95 us a step of both and 2 us:  8192 x 1024 -> 1024 256 18.8, 128 14.5;  4096 x 1024 -> 4096 256 21.8, 128 24.5;
 //     16384 x 4096 -> 4096 256 207, 128 255.  fp32 results have no 256 x 256 tiles (the exact way needs the registers).
 inline int64_t linear8_groups(int64_t n, int64_t d_out, int64_t tokens, int64_t outputs) {
     return ((n + tokens - 1) / tokens) * ((d_out + outputs - 1) / outputs);
@@ -41,12 +46,14 @@ inline int linear8_plan(int64_t n, int64_t d_in, int64_t d_out, int64_t ld_x, in
     if (linear8_groups(n, d_out, 16, 16) <= kUnits) return LINEAR8_FEW_16x16;
     if (linear8_groups(n, d_out, 16, 32) <= kUnits) return LINEAR8_FEW_16x32;
     if (linear8_groups(n, d_out, 32, 32) <= kUnits) return LINEAR8_FEW_32x32;
+    const int64_t steps = (d_in + 127) / 128;
+    if (n > 16 && steps <= 8 && linear8_groups(n, d_out, 32, 32) <= 2 * kUnits) return LINEAR8_MANY_32x32;
     if (linear8_groups(n, d_out, 64, 32) <= kUnits) return LINEAR8_FEW_64x32;
     if (n <= 16) return LINEAR8_MANY_16x64;
     const int64_t small = linear8_groups(n, d_out, 128, 128), large = linear8_groups(n, d_out, 256, 256);
     const bool fits = ld_x < (1 << 23) && ld_w < (1 << 23) && small < (1 << 23);  // (offsets within a tile, and the grid, in 32 bits)
     if (n <= 32 || !fits) return LINEAR8_MANY_32x32;
-    const int64_t steps = (d_in + 127) / 128;
+    if (n <= 64 || linear8_groups(n, d_out, 64, 32) <= 2 * kUnits) return LINEAR8_MANY_64x32;
     if (linear8_groups(n, d_out, 64, 128) <= kUnits && steps >= (exact ? 3 : 6)) return LINEAR8_TILE_64x128;
     if (small <= kUnits && steps >= 20) return LINEAR8_TILE_128_SPLIT;
     if (exact) return LINEAR8_TILE_128;

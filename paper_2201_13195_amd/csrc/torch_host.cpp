@@ -418,7 +418,7 @@ Pair8 new_mat8(const Tensor &like, int64_t rows, int64_t cols, bool weights, at:
     p.m = {p.data.data_ptr(), ld, p.scales.data_ptr(), lds, f8_code(f8), scale_code(scale)};
     return p;
 }
-// The descriptor of given tensors (anything unusual about them is for binding.py to judge).
+// The descriptor of given tensors (anything unusual about them is left to binding.py).
 rmm_mat8_t old_mat8(const Tensor &data, const Tensor &scales, bool weights, const Tensor &like) {
     need(data.is_cuda() && scales.is_cuda() && data.device() == like.device() && scales.device() == like.device());
     need(data.dim() == 2 && scales.dim() == 2 && f8_code(data.scalar_type()) >= 0 && scale_code(scales.scalar_type()) >= 0);

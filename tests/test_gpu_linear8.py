@@ -184,7 +184,9 @@ def test_large_offsets():
     assert torch.equal(Y[-300:, :128], first[-300:]) and torch.equal(Y[-300:, 128 * 200:128 * 201], first[-300:])
 
 
-TILES = [(2100, 999, 520), (300, 1000, 3001), (3000, 2501, 1000), (2100, 300, 1500), (4300, 1001, 4090)]     # 64 x 128 twice, 128 split, 128, 256
+# kernels: 64x32, 64 x 128 tiles twice, 128 split, 128, 256; then those of few tokens
+TILES = [(300, 1000, 3001), (2100, 999, 520), (300, 1000, 3501), (3000, 2501, 1000), (2100, 300, 1500), (4300, 1001, 4090),
+         (5, 1001, 3000), (40, 2001, 1001), (128, 1111, 4000), (16, 1001, 9000), (30, 2001, 9000), (60, 1001, 9000)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])

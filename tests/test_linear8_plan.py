@@ -6,7 +6,7 @@ import subprocess
 import pytest
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2201_13195_amd", "csrc")
-FEW_16x16, FEW_16x32, FEW_32x32, FEW_64x32, MANY_16x64, MANY_32x32, TILE_64x128, TILE_128_SPLIT, TILE_128, TILE_256 = range(10)
+FEW_16x16, FEW_16x32, FEW_32x32, FEW_64x32, MANY_16x64, MANY_32x32, MANY_64x32, TILE_64x128, TILE_128_SPLIT, TILE_128, TILE_256 = range(11)
 UNITS = 256
 
 # (n, d_in, d_out) of each kernel, bf16 and fp32 results; tests/test_gpu_linear8.py runs them.
@@ -14,10 +14,10 @@ KERNELS = [
     ((5, 200, 70), FEW_16x16, FEW_16x16), ((256, 512, 256), FEW_16x16, FEW_16x16),
     ((16, 1000, 5000), FEW_16x32, FEW_16x32), ((130, 777, 800), FEW_16x32, FEW_16x32),
     ((60, 300, 3001), FEW_32x32, FEW_32x32), ((500, 900, 510), FEW_32x32, FEW_32x32),
-    ((333, 1000, 1111), FEW_64x32, FEW_64x32), ((128, 2048, 4000), FEW_64x32, FEW_64x32),
+    ((333, 1000, 1111), MANY_32x32, MANY_32x32), ((333, 1030, 1111), FEW_64x32, FEW_64x32), ((128, 2048, 4000), FEW_64x32, FEW_64x32),
     ((1, 520, 9001), MANY_16x64, MANY_16x64), ((16, 136, 20000), MANY_16x64, MANY_16x64),
     ((20, 520, 9001), MANY_32x32, MANY_32x32), ((32, 131, 17000), MANY_32x32, MANY_32x32),
-    ((600, 400, 1200), TILE_128, TILE_64x128), ((1100, 2050, 1030), TILE_64x128, TILE_64x128),
+    ((600, 400, 1200), MANY_64x32, MANY_64x32), ((50, 777, 17000), MANY_64x32, MANY_64x32), ((256, 2100, 4001), MANY_64x32, MANY_64x32), ((1100, 2050, 1030), TILE_64x128, TILE_64x128),
     ((500, 777, 3000), TILE_64x128, TILE_64x128),     # seven blocks: the second group has none in the last step
     ((260, 1160, 4090), TILE_64x128, TILE_64x128), ((100, 1111, 9000), TILE_64x128, TILE_64x128),
     ((900, 2600, 4000), TILE_128_SPLIT, TILE_128_SPLIT), ((2000, 2440, 2040), TILE_128_SPLIT, TILE_128_SPLIT),
@@ -53,20 +53,25 @@ def test_kernels_by_shape(plan, shape, bf16, f32):
 
 
 def test_every_kernel_is_among_them():
-    assert {k for _, k, _ in KERNELS} == set(range(10))
+    assert {k for _, k, _ in KERNELS} == set(range(11))
 
 
-def test_few_outputs_never_take_more_than_a_round(plan):
+def test_few_outputs_take_the_kernels_without_tiles(plan):
     for n in (1, 2, 15, 16, 17, 31, 33, 64, 65, 100, 128, 200, 333, 512, 1000, 2048):
-        for d_out in (1, 16, 17, 100, 128, 700, 1024, 1111, 2048, 4096, 5000, 8192, 9000):
-            k = plan(n, 1024, d_out)
-            sizes = {FEW_16x16: (16, 16), FEW_16x32: (16, 32), FEW_32x32: (32, 32), FEW_64x32: (64, 32)}
-            if k in sizes:
-                assert groups(n, d_out, *sizes[k]) <= UNITS
-                assert all(groups(n, d_out, *sizes[j]) > UNITS for j in sizes if j < k)          # the smallest that does
-            else:
-                assert groups(n, d_out, 64, 32) > UNITS
-                assert (k == MANY_16x64) == (n <= 16) and (k == MANY_32x32) == (16 < n <= 32)
+        for d_in in (100, 1024, 1030, 4096):
+            for d_out in (1, 16, 17, 100, 128, 700, 1024, 1111, 2048, 4096, 5000, 8192, 9000, 20000):
+                k, short = plan(n, d_in, d_out), d_in <= 1024
+                sizes = {FEW_16x16: (16, 16), FEW_16x32: (16, 32), FEW_32x32: (32, 32), FEW_64x32: (64, 32)}
+                fit = [j for j in sorted(sizes) if groups(n, d_out, *sizes[j]) <= UNITS]
+                two = n > 16 and short and groups(n, d_out, 32, 32) <= 2 * UNITS
+                if fit and not (fit[0] == FEW_64x32 and two):
+                    assert k == fit[0]                              # the smallest that is one round of work-groups
+                elif n <= 16:
+                    assert k == MANY_16x64
+                elif n <= 32 or two:
+                    assert k == MANY_32x32
+                else:
+                    assert (k == MANY_64x32) == (n <= 64 or groups(n, d_out, 64, 32) <= 2 * UNITS)
 
 
 def test_groups_that_share_the_contraction_have_a_compute_unit_each(plan):
@@ -96,4 +101,4 @@ def test_operands_beyond_32_bits_of_a_tile(plan):
         for d in (1, 1000, (1 << 31) - 1):
             for o in (1, 1000, (1 << 31) - 1):
                 if n * d < 1 << 40 and n * o < 1 << 40 and d * o < 1 << 40:
-                    assert 0 <= plan(n, d, o) < 10 and 0 <= plan(n, d, o, exact=True) < TILE_256
+                    assert 0 <= plan(n, d, o) <= TILE_256 and 0 <= plan(n, d, o, exact=True) < TILE_256
