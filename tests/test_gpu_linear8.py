@@ -274,3 +274,21 @@ def test_every_tile_kernel_in_a_graph_replayed():
         torch.cuda.synchronize()
         for a, b, c, d in zip(want, out, again, run_here):
             assert torch.equal(a, b) and torch.equal(a, c) and torch.equal(a, d)
+
+
+def test_more_tiles_than_a_launch_has_work_groups():
+    """2^30 tokens of one block: the work-groups go on from tile to tile."""
+    n, d_in, d_out = (1 << 30) + 37, 16, 3
+    data = torch.randint(0, 0x60, (1 << 20, 16), dtype=torch.uint8, device=DEV, generator=torch.Generator(DEV).manual_seed(1))
+    X = torch.empty((n, 16), dtype=torch.uint8, device=DEV)
+    for at in range(0, n, 1 << 20):
+        here = min(1 << 20, n - at)
+        X[at:at + here] = data[:here] ^ ((at >> 20) & 3)
+    xs = torch.full((1, (n + 15) // 16 * 16), 127, dtype=torch.uint8, device=DEV)[:, :n]
+    xs[0, 5::7] = 126
+    w = rmm.rmm_quantize8_weight(torch.randn(d_out, d_in, device=DEV), scale_dtype=torch.float8_e8m0fnu)
+    Y = rmm.rmm_linear8(X.view(E4), xs.view(torch.float8_e8m0fnu), *w)
+    for at in (0, (1 << 22) * 32 - 160, (1 << 27) + 64, (1 << 29) + 48, (1 << 30) - 2000):
+        part = slice(at, min(at + 2048, n))
+        want = rmm.rmm_linear8(X[part].view(E4), xs[:, part].view(torch.float8_e8m0fnu), *w)
+        assert torch.equal(Y[part], want)
