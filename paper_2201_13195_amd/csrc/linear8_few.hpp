@@ -6,7 +6,8 @@
 // sums are added at the end, in the order of the waves.
 //   fragments loaded from memory as the matrix instruction wants them (a quarter of a wave's addresses in 16 lines): 1 x 4096 -> 4096
 //   5.1 us, 24 x 4096 -> 1024 6.2, 64 x 4096 -> 4096 10.4, 128 x 4096 -> 4096 14.7; like this 4.5, 4.2, 7.0, 8.0
-//   two and three blocks of a wave on their way instead of one: 4.5 and 4.7, 4.4 and 4.6 us; LDS then holds fewer work-groups
+//   two and three blocks of a wave on their way: 1 x 4096 -> 4096 4.5 and 4.7 us (one: 4.6), 24 x 4096 -> 1024 4.4 and 4.6 (4.2),
+//   1 x 1024 -> 4096 3.6 (3.3): more code, and LDS holds fewer work-groups
 #pragma once
 #include "lds_loads.hpp"
 #include "linear8_frag.hpp"
