@@ -212,7 +212,8 @@ struct NormBackwardArgs {
 };
 
 // What is read of a row; that of the next row is requested before this one is reduced (not with two runs a lane in 16 waves, 128
-// registers each: there are enough requests between them).  4096 x 8192 bf16: one run a lane 57 us, two, half of the lanes idle, 73.
+// registers each: there are enough requests between them).  4096 x 8192 bf16, 512 work-groups: one run a lane 57 us, two, half of the lanes
+// idle, 73.
 template <typename T, int CH>
 struct BackwardRow {
     Run8<T> dy[CH], h[CH], dh[CH];
@@ -392,14 +393,17 @@ __global__ void __launch_bounds__(1024) sum_parts_kernel(const float *__restrict
 // Columns that CH runs a lane in WPR waves hold.
 constexpr int64_t columns(int ch, int wpr) { return (int64_t)ch * wpr * 64 * kRun; }
 int64_t rows_a_group(int64_t d) { return d <= columns(2, 1) ? 4 : 1; }
-constexpr int64_t kMostForward = 2048, kMostBackward = 512;  // work-groups: eight, two for each compute unit
+constexpr int64_t kMostForward = 2048;  // work-groups: eight for each compute unit
+// Two, or the one of 16 waves that its registers hold (each has a row of partial sums of dw: 4096 x 8192 bf16 45.8 us, with two 56.1; with one of
+// four waves 16384 x 4096 113.8, with two 101.1, with three 107.6).
+int64_t most_backward(int64_t d) { return d <= columns(2, 4) ? 512 : 256; }
 // (four runs a lane in 16 waves are more than their registers hold: with 8-bit rows, 1000 x 32768 bf16 85 us, read twice 62; 2048 x 16384
 // with four runs 134, with two 58)
 bool long_rows(int64_t d) { return d > columns(2, 16); }
 int64_t backward_groups(int64_t n, int64_t d) {
-    if (long_rows(d)) return n < 16 ? n : 16;
+    if (long_rows(d)) return n < 64 ? n : 64;
     const int64_t groups = (n + rows_a_group(d) - 1) / rows_a_group(d);
-    return groups < kMostBackward ? groups : kMostBackward;
+    return groups < most_backward(d) ? groups : most_backward(d);
 }
 
 }  // namespace
