@@ -346,8 +346,8 @@ __global__ void __launch_bounds__(1024) rms_norm_backward_long_kernel(NormBackwa
     }
 }
 
-// Partial sums of dw where the rows are too long: work-group (x, y) takes 512 columns, every gridDim.y-th row of four
-// waves.  Runs before dX is written (it may be the buffer of dY).
+// Partial sums of dw where the rows are too long: work-group (x, y) takes 512 columns of every gridDim.y-th row.
+// Runs before dX is written (it may be the buffer of dY).
 template <typename T>
 __global__ void __launch_bounds__(64) rms_norm_dweight_kernel(NormBackwardArgs g) {
     for (int64_t c0 = (int64_t)blockIdx.x * 512; c0 < g.d; c0 += (int64_t)gridDim.x * 512) {
