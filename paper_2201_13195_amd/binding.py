@@ -131,6 +131,12 @@ def _native(name, *args):
     return r
 
 
+def watched(*tensors):
+    """Whether a call on these tensors (None among them) is being traced, carries forward-mode tangents or stands inside a function
+    transform: what makes its outputs without torch operators would go unseen there, so that it must be a Python autograd function."""
+    return (_HOST or host()).watched(*tensors)
+
+
 def rmm_version():
     return load_library().rmm_version()
 

@@ -317,9 +317,20 @@ PyObject *py_variance_stats(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
 bool watched(const Tensor &t) {
     return t.defined() && (t._fw_grad(/*level=*/0).defined() || !t.has_storage());
 }
+bool all_watched() {
+    return torch::jit::tracer::isTracing() || c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode);
+}
 void need_unwatched(const Tensor &X, const Tensor &W, const Tensor &bias) {
-    need(!torch::jit::tracer::isTracing() && !watched(X) && !watched(W) && !watched(bias) &&
-         !c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode));
+    need(!all_watched() && !watched(X) && !watched(W) && !watched(bias));
+}
+
+// watched(tensors or None ..) -> bool
+PyObject *py_watched(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    bool yes = all_watched();
+    for (Py_ssize_t i = 0; i < nargs && !yes; ++i) yes = THPVariable_Check(a[i]) && watched(THPVariable_Unpack(a[i]));
+    return PyBool_FromLong(yes);
+    END_HANDLE_TH_ERRORS
 }
 
 // X as a dense n x d_in matrix
@@ -560,7 +571,8 @@ PyObject *py_rms_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t nargs)
 #define RMM_METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_##NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RMM_METHOD(forward), RMM_METHOD(backward), RMM_METHOD(sketch), RMM_METHOD(variance_stats),
                          RMM_METHOD(linear),  RMM_METHOD(infer),    RMM_METHOD(quantize8), RMM_METHOD(quantize8_weight),
-                         RMM_METHOD(linear8), RMM_METHOD(rms_norm), RMM_METHOD(rms_norm_backward), {nullptr, nullptr, 0, nullptr}};
+                         RMM_METHOD(linear8), RMM_METHOD(rms_norm), RMM_METHOD(rms_norm_backward), RMM_METHOD(watched),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rmm_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 PyTypeObject node_type;

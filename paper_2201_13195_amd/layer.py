@@ -201,6 +201,15 @@ class RMMLinear8Function(torch.autograd.Function):
         return (dX, None, None, dW if ctx.needs_input_grad[3] else None, db) + (None,) * 6
 
 
+class RMMInfer8Function(torch.autograd.Function):
+    """RMMLinear8's n x d_out result alone, as a call that a trace records and that refuses forward-mode tangents.  (W: for the tangent
+    that it may have, and the parameter of a traced copy.)"""
+
+    @staticmethod
+    def forward(ctx, X, data, scales, W, bias, layer):
+        return layer._infer(X, data, scales, W, bias)
+
+
 class RMMLinear8(RMMLinear):
     """RMMLinear with Y and dX as products of 8-bit operands: X, dY in rows with a scale for each 128 columns, W with one for each
     128 x 128 block, made anew from W in every call; the weight gradient is RMMLinear's sketched estimate.  Takes a tensor, or the
@@ -225,13 +234,18 @@ class RMMLinear8(RMMLinear):
         self._packed = (binding.rmm_quantize8_weight(W.contiguous(), scale_dtype=self.scale_dtype), self.weight, self.weight._version)
         return self
 
-    def _weight8(self):
+    def _weight8(self, W):
         if self._packed is None:
-            return binding.rmm_quantize8_weight(self.weight.detach().contiguous(), scale_dtype=self.scale_dtype)
+            return binding.rmm_quantize8_weight(W.detach().contiguous(), scale_dtype=self.scale_dtype)
         w8, of, version = self._packed
         if of is not self.weight or version != self.weight._version:
             raise RuntimeError("RMMLinear8: the weight has changed since pack(); call pack() again")
         return w8
+
+    def _infer(self, X, data, scales, W, bias):
+        if data is None:
+            data, scales = binding.rmm_quantize8(_rows(X), scale_dtype=self.scale_dtype)
+        return binding.rmm_linear8(data, scales, *self._weight8(W), None if bias is None else bias.detach(), W.dtype)
 
     def forward(self, X):
         rows = X if isinstance(X, Rows8) else None
@@ -241,13 +255,11 @@ class RMMLinear8(RMMLinear):
         if full is not None and full.dtype != self.weight.dtype:
             raise TypeError("RMMLinear8: X must have the weight's dtype, %s, has %s" % (self.weight.dtype, full.dtype))
         if not torch.is_grad_enabled():
-            if rows is None:
-                lead = X.shape[:-1]
-                data, scales = binding.rmm_quantize8(_rows(X), scale_dtype=self.scale_dtype)
-            else:
-                data, scales, lead = rows.data, rows.scales, rows.lead
-            bias = None if self.bias is None else self.bias.detach()
-            return binding.rmm_linear8(data, scales, *self._weight8(), bias, self.weight.dtype).reshape(*lead, self.out_features)
+            lead = X.shape[:-1] if rows is None else rows.lead
+            args = (X, None, None) if rows is None else (None, rows.data, rows.scales)
+            args += (self.weight, self.bias)
+            Y = RMMInfer8Function.apply(*args, self) if binding.watched(*args) else self._infer(*args)
+            return Y.reshape(*lead, self.out_features)
         if rows is not None:
             if rows.Y is None:
                 raise ValueError("RMMLinear8: these rows were made without gradients; a backward pass needs them in the layer's dtype too")

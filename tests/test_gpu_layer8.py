@@ -1,6 +1,7 @@
 """GPU: RMMNorm and RMMLinear8 under autograd, the operators one after the other, streams and graphs."""
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 import eight
 import paper_2201_13195_amd as rmm
@@ -243,3 +244,53 @@ def test_packed_weights_that_changed_are_refused():
         with pytest.raises(RuntimeError, match="has changed"):
             layer(X)
         assert torch.equal(layer.pack()(X), 2 * want)
+
+
+class Block(torch.nn.Module):
+    def __init__(self, norm, lin):
+        super().__init__()
+        self.norm, self.lin = norm, lin
+
+    def forward(self, X, R):
+        return block(self.norm, self.lin, X, R)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_calls_without_gradients_are_traced_and_refuse_tangents(packed):
+    lin = rmm.RMMLinear8(64, 24, k=20, seed=3, layer_id=1)
+    norm = rmm.RMMNorm(64, f8=E4, scale_dtype=torch.float8_e8m0fnu)
+    X, X2, R = (torch.randn(3, 10, 64, device=DEV, dtype=torch.bfloat16) for _ in range(3))
+    both = Block(norm, lin)
+    with torch.no_grad():
+        if packed:
+            lin.pack()
+        traced = torch.jit.trace(lin, (X,), check_trace=False)
+        for x in (X, X2, X2.reshape(5, 6, 64)):
+            assert torch.equal(traced(x), lin(x))
+        traced = torch.jit.trace(both, (X, R), check_trace=False)
+        for x in (X, X2, X2.reshape(5, 6, 64)):
+            assert all(torch.equal(a, b) for a, b in zip(traced(x, R.reshape(x.shape)), both(x, R.reshape(x.shape))))
+        with forward_ad.dual_level():
+            dual = forward_ad.make_dual(X, torch.ones_like(X))
+            for call in (lambda: lin(dual), lambda: norm(dual), lambda: both(X, dual)):
+                with pytest.raises(NotImplementedError):
+                    call()
+        for f in (lin, rmm.RMMNorm(64)):
+            with pytest.raises(RuntimeError):
+                torch.vmap(f)(X)
+    assert lin.calls == 0
+
+
+def test_tracing_records_the_norm_and_the_layer():
+    """With gradients too, as the layer in bf16 does."""
+    lin = rmm.RMMLinear8(64, 24, k=20, seed=3, layer_id=1)
+    both = Block(rmm.RMMNorm(64, f8=E4, scale_dtype=torch.float8_e8m0fnu), lin)
+    X, X2, R = (torch.randn(30, 64, device=DEV, dtype=torch.bfloat16) for _ in range(3))
+    traced = torch.jit.trace(both, (X, R), check_trace=False)
+    for x in (X, X2):
+        lin.calls = 0
+        params = (both.norm.weight, lin.weight, lin.bias)
+        got, want = traced(x, R), both(x, R)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        for a, b in zip(*(torch.autograd.grad(y.float().sum() + h.float().sum(), params) for y, h in (got, want))):
+            assert torch.equal(a, b)
