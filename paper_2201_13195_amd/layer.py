@@ -114,9 +114,18 @@ class Rows8(NamedTuple):
     lead: Tuple[int, ...]             # the leading sizes that the n rows stand for
 
 
+def _dense(t):
+    """t (or None) as the library takes it: contiguous, from a multiple of 16 bytes on.  (A slice of rows of odd width, which the backward
+    pass of a cat hands on too, or a parameter in a flat one may be contiguous and start anywhere.)"""
+    if t is None:
+        return None
+    if not t.is_contiguous():
+        t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
 def _rows(X):
-    X = X.reshape(-1, X.shape[-1])
-    return X if X.is_contiguous() else X.contiguous()
+    return None if X is None else _dense(X.reshape(-1, X.shape[-1]))
 
 
 class RMMNormFunction(torch.autograd.Function):
@@ -124,7 +133,7 @@ class RMMNormFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, X, residual, weight, eps, f8, scale_dtype, need_Y):
-        r = binding.rmm_rms_norm(_rows(X), weight.contiguous(), None if residual is None else _rows(residual), eps, need_Y, f8, scale_dtype)
+        r = binding.rmm_rms_norm(_rows(X), _dense(weight), _rows(residual), eps, need_Y, f8, scale_dtype)
         ctx.set_materialize_grads(False)
         H = X if residual is None else r.H.reshape(X.shape)
         ctx.save_for_backward(H, weight, r.rstd)
@@ -141,8 +150,7 @@ class RMMNormFunction(torch.autograd.Function):
         if dY is not None:
             need_dX, need_dw = ctx.needs_input_grad[0] or ctx.needs_input_grad[1], ctx.needs_input_grad[2]
             if need_dX or need_dw:
-                dX, dweight = binding.rmm_rms_norm_backward(_rows(dY), _rows(H), weight.contiguous(), rstd, None if dH is None else _rows(dH),
-                                                            need_dX, need_dw)
+                dX, dweight = binding.rmm_rms_norm_backward(_rows(dY), _rows(H), _dense(weight), rstd, _rows(dH), need_dX, need_dw)
             dX = None if dX is None else dX.reshape(H.shape)
         return dX, dX if ctx.has_residual else None, dweight, None, None, None, None
 
@@ -174,11 +182,11 @@ class RMMLinear8Function(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, X, data, scales, W, bias, k, kind, seed, offset, scale_dtype, grad_f8):
-        X2, Wc = _rows(X), W.contiguous()
+        X2, Wc = _rows(X), _dense(W)
         if data is None:
             data, scales = binding.rmm_quantize8(X2, scale_dtype=scale_dtype)
         w8, w_scales = binding.rmm_quantize8_weight(Wc, scale_dtype=scale_dtype)
-        Y = binding.rmm_linear8(data, scales, w8, w_scales, bias, X.dtype)
+        Y = binding.rmm_linear8(data, scales, w8, w_scales, _dense(bias), X.dtype)
         X_proj = binding.rmm_sketch(X2, k, kind, seed, offset)
         ctx.save_for_backward(Wc, X_proj)
         ctx.state, ctx.formats = (kind, seed, offset), (scale_dtype, grad_f8)
@@ -231,12 +239,12 @@ class RMMLinear8(RMMLinear):
 
     def pack(self):
         W = self.weight.detach()
-        self._packed = (binding.rmm_quantize8_weight(W.contiguous(), scale_dtype=self.scale_dtype), self.weight, self.weight._version)
+        self._packed = (binding.rmm_quantize8_weight(_dense(W), scale_dtype=self.scale_dtype), self.weight, self.weight._version)
         return self
 
     def _weight8(self, W):
         if self._packed is None:
-            return binding.rmm_quantize8_weight(W.detach().contiguous(), scale_dtype=self.scale_dtype)
+            return binding.rmm_quantize8_weight(_dense(W.detach()), scale_dtype=self.scale_dtype)
         w8, of, version = self._packed
         if of is not self.weight or version != self.weight._version:
             raise RuntimeError("RMMLinear8: the weight has changed since pack(); call pack() again")
@@ -245,7 +253,7 @@ class RMMLinear8(RMMLinear):
     def _infer(self, X, data, scales, W, bias):
         if data is None:
             data, scales = binding.rmm_quantize8(_rows(X), scale_dtype=self.scale_dtype)
-        return binding.rmm_linear8(data, scales, *self._weight8(W), None if bias is None else bias.detach(), W.dtype)
+        return binding.rmm_linear8(data, scales, *self._weight8(W), _dense(None if bias is None else bias.detach()), W.dtype)
 
     def forward(self, X):
         rows = X if isinstance(X, Rows8) else None

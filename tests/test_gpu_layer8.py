@@ -294,3 +294,20 @@ def test_tracing_records_the_norm_and_the_layer():
         assert all(torch.equal(a, b) for a, b in zip(got, want))
         for a, b in zip(*(torch.autograd.grad(y.float().sum() + h.float().sum(), params) for y, h in (got, want))):
             assert torch.equal(a, b)
+
+
+def test_slices_and_gradients_that_start_anywhere():
+    """Rows of odd widths: a slice, and the gradient that the backward pass of a cat hands on, start off the library's 16 bytes."""
+    torch.manual_seed(9)
+    for m, d in ((rmm.RMMNorm(1001, dtype=torch.float32), 1001), (rmm.RMMLinear8(1001, 77, k=2, dtype=torch.float32), 77)):
+        whole, dY = torch.randn(7, 1001, device=DEV, requires_grad=True), torch.randn(7, d, device=DEV)
+        assert whole[3:].data_ptr() % 16 and (3 * d * 4) % 16
+        m.calls = 0                                       # (the same sketches both times)
+        y = torch.cat([m(whole[:3]), m(whole[3:])])
+        got = torch.autograd.grad(y, [whole, m.weight], dY)
+        m.calls = 0
+        ya, yb = m(whole[:3].clone()), m(whole[3:].clone())
+        want = torch.autograd.grad([ya, yb], [whole, m.weight], [dY[:3].clone(), dY[3:].clone()])
+        assert torch.equal(y, torch.cat([ya, yb])) and all(torch.equal(a, b) for a, b in zip(got, want))
+        with torch.no_grad():
+            assert torch.equal(m(whole[3:]), yb)

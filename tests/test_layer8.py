@@ -19,6 +19,13 @@ def number(t):
     return t.detach().float().numpy()
 
 
+def take(*tensors):
+    """What the library checks of its operands."""
+    for t in tensors:
+        if t is not None and (not t.is_contiguous() or t.data_ptr() % 16):
+            raise binding.RmmError(-1, "stand-in")
+
+
 @pytest.fixture
 def stand_ins(monkeypatch):
     """Rows and weights stay what they are, scales are ones; the calls made so far, by name."""
@@ -26,31 +33,49 @@ def stand_ins(monkeypatch):
 
     def quantize8(A, f8=E4, scale_dtype=torch.float32):
         calls.append("quantize8")
+        take(A)
         return opaque(number(A).copy()), torch.ones(binding._blocks8(A.shape[1]), A.shape[0]).to(scale_dtype)
 
     def quantize8_weight(W, f8=E4, scale_dtype=torch.float32, transposed=False):
         calls.append("quantize8_weight")
+        take(W)
         scales = torch.ones(binding._blocks8(W.shape[0]), binding._blocks8(W.shape[1])).to(scale_dtype)
         return (opaque(number(W).copy()), scales) + ((opaque(number(W).T.copy()), scales.t()) if transposed else ())
 
     def linear8(X8, x_scales, W8, w_scales, bias=None, dtype=torch.bfloat16, Y=None):
         calls.append("linear8")
+        take(bias)
         return opaque(number(X8) @ number(W8).T + (0 if bias is None else number(bias))).to(dtype)
 
     def sketch(A, k, kind, seed, offset):
         calls.append("sketch")
+        take(A)
         return opaque(number(A)[:k].copy()).to(A.dtype)
 
     def rms_norm(X, weight, residual=None, eps=1e-6, need_Y=True, f8=None, scale_dtype=torch.float32):
         calls.append("rms_norm")
+        take(X, weight, residual)
         h = number(X) + (0 if residual is None else number(residual))
         rstd = 1 / np.sqrt((h * h).mean(1) + eps)
         y = h * rstd[:, None] * number(weight)
         rows = quantize8(opaque(y), f8, scale_dtype) if f8 is not None else (None, None)
         return binding.RMSNormResult(opaque(y).to(X.dtype) if need_Y else None, X if residual is None else opaque(h).to(X.dtype), opaque(rstd), *rows)
 
+    def rms_norm_backward(dY, H, weight, rstd, dH=None, need_dX=True, need_dweight=True):
+        calls.append("rms_norm_backward")
+        take(dY, H, weight, dH)
+        r = rstd[:, None].double()
+        g, hat = dY.double() * weight.double(), H.double() * r
+        dX = r * (g - hat * (g * hat).mean(1, keepdim=True)) + (0 if dH is None else dH)
+        return dX.to(H.dtype), (dY * hat).sum(0).to(H.dtype)
+
+    def backward(dY, W, X_proj, kind, seed, offset, need_dX=True, need_dbias=False):
+        calls.append("backward")
+        take(dY, W, X_proj)
+        return None, opaque(number(dY)[:X_proj.shape[0]].T @ number(X_proj)), opaque(number(dY).sum(0))
+
     for name, f in (("rmm_quantize8", quantize8), ("rmm_quantize8_weight", quantize8_weight), ("rmm_linear8", linear8), ("rmm_sketch", sketch),
-                    ("rmm_rms_norm", rms_norm)):
+                    ("rmm_rms_norm", rms_norm), ("rmm_rms_norm_backward", rms_norm_backward), ("rmm_backward", backward)):
         monkeypatch.setattr(binding, name, f)
     return calls
 
@@ -102,3 +127,50 @@ def test_the_norm_with_the_layer_behind_it_is_traced(stand_ins):
         rows, _ = norm(X, R)
         with forward_ad.dual_level(), pytest.raises(NotImplementedError):
             lin(rows._replace(data=forward_ad.make_dual(rows.data, torch.ones_like(rows.data))))
+
+
+def off_16(*shape):
+    """A dense tensor that starts 4 bytes behind a multiple of 16."""
+    n = int(np.prod(shape))
+    t = torch.randn(n + 1)[1:].view(*shape)
+    assert t.is_contiguous() and t.data_ptr() % 16 == 4
+    return t
+
+
+def test_tensors_that_start_anywhere(stand_ins):
+    """Slices of rows of odd width are dense and start off the library's 16 bytes; a cat's backward hands such a gradient on."""
+    norm = rmm.RMMNorm(15, device="cpu", dtype=torch.float32)
+    lin = rmm.RMMLinear8(15, 13, device="cpu", dtype=torch.float32, k=4)
+    for m, d in ((norm, 15), (lin, 13)):
+        whole = torch.randn(7, 15, requires_grad=True)
+        a, b = whole[:3], whole[3:]
+        assert b.is_contiguous() and b.data_ptr() % 16
+        dY = torch.randn(7, d)
+        y = torch.cat([m(a), m(b)])
+        y.backward(dY)
+        grad, whole.grad = whole.grad, None
+        ya, yb = m(whole[:3].clone()), m(whole[3:].clone())
+        assert torch.equal(y, torch.cat([ya, yb]))
+        torch.autograd.backward([ya, yb], [dY[:3].clone(), dY[3:].clone()])
+        assert torch.equal(whole.grad, grad)
+        with torch.no_grad():
+            assert torch.equal(m(off_16(5, 15).copy_(whole[:5])), m(whole[:5].clone()))
+    X, R, dH = off_16(5, 15).requires_grad_(True), off_16(5, 15), off_16(5, 15)
+    Y, H = norm(X, R)
+    torch.autograd.backward([Y, H], [off_16(5, 15), dH])
+    assert X.grad.shape == X.shape
+
+
+def test_parameters_that_start_anywhere(stand_ins):
+    """Views into one flat tensor, as sharding programs make them of parameters."""
+    norm = rmm.RMMNorm(16, device="cpu", dtype=torch.float32)
+    lin = layer()
+    X = torch.randn(5, 16)
+    want = lin(norm(X)).detach()
+    norm.weight.data = off_16(16).copy_(norm.weight.data)
+    lin.weight.data, lin.bias.data = off_16(12, 16).copy_(lin.weight.data), off_16(12).copy_(lin.bias.data)
+    out = lin(norm(X))
+    out.sum().backward()
+    assert torch.equal(out, want) and lin.weight.grad is not None and norm.weight.grad is not None
+    with torch.no_grad():
+        assert torch.equal(lin(norm(X)), want) and torch.equal(lin.pack()(norm(X)), want)
