@@ -158,9 +158,9 @@ class RMMNormFunction(torch.autograd.Function):
 class RMMNorm(torch.nn.Module):
     """Root-mean-square norm over the last dimension: Y = H / sqrt(mean H^2 + eps) * weight, H = X (+ residual).
     `norm(X)` returns Y, `norm(X, residual)` returns (Y, H).  With `f8` (a float8 dtype) Y comes as Rows8, which RMMLinear8 takes
-    as it is: the 8-bit rows cost no pass of their own."""
+    as it is (both have powers of two as their default scales): the 8-bit rows cost no pass of their own."""
 
-    def __init__(self, features, eps=1e-6, f8=None, scale_dtype=torch.float32, device="cuda", dtype=torch.bfloat16):
+    def __init__(self, features, eps=1e-6, f8=None, scale_dtype=torch.float8_e8m0fnu, device="cuda", dtype=torch.bfloat16):
         super().__init__()
         self.eps, self.f8, self.scale_dtype = float(eps), f8, scale_dtype
         self.weight = torch.nn.Parameter(torch.ones((features,), device=device, dtype=dtype))
@@ -262,6 +262,8 @@ class RMMLinear8(RMMLinear):
         full = X if rows is None else rows.Y
         if full is not None and full.dtype != self.weight.dtype:
             raise TypeError("RMMLinear8: X must have the weight's dtype, %s, has %s" % (self.weight.dtype, full.dtype))
+        if rows is not None and rows.scales.dtype != self.scale_dtype:
+            raise TypeError("RMMLinear8: rows with scales of %s, the layer's scale_dtype is %s" % (rows.scales.dtype, self.scale_dtype))
         if not torch.is_grad_enabled():
             lead = X.shape[:-1] if rows is None else rows.lead
             args = (X, None, None) if rows is None else (None, rows.data, rows.scales)

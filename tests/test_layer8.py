@@ -174,3 +174,20 @@ def test_parameters_that_start_anywhere(stand_ins):
     assert torch.equal(out, want) and lin.weight.grad is not None and norm.weight.grad is not None
     with torch.no_grad():
         assert torch.equal(lin(norm(X)), want) and torch.equal(lin.pack()(norm(X)), want)
+
+
+def test_defaults_of_the_two_modules_fit_together(stand_ins):
+    norm, lin = rmm.RMMNorm(16, f8=E4, device="cpu", dtype=torch.float32), layer()
+    assert norm.scale_dtype == lin.scale_dtype
+    assert torch.isfinite(lin(norm(torch.randn(5, 16)))).all()
+
+
+@pytest.mark.parametrize("gradients", [False, True])
+def test_rows_with_another_kind_of_scales_are_refused_before_anything_happens(stand_ins, gradients):
+    norm, lin = rmm.RMMNorm(16, f8=E4, scale_dtype=torch.float32, device="cpu", dtype=torch.float32), layer()
+    with torch.set_grad_enabled(gradients):
+        rows = norm(torch.randn(5, 16))
+        del stand_ins[:]
+        with pytest.raises(TypeError, match="scale_dtype"):
+            lin(rows)
+    assert lin.calls == 0 and not stand_ins
