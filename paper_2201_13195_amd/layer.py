@@ -225,7 +225,7 @@ class RMMLinear8(RMMLinear):
     `grad_f8`: the format of dY's rows.
 
     pack() keeps W's 8-bit form for calls without gradients, until W changes: such a call refuses then (a change through
-    weight.data, which torch does not count, goes unnoticed)."""
+    weight.data, which torch does not count, goes unnoticed).  Copies of the layer, and what .to() makes of it, are not packed."""
 
     def __init__(self, in_features, out_features, bias=True, rho=0.1, k=None, kind=binding.GAUSSIAN, seed=0, layer_id=None,
                  device="cuda", dtype=torch.bfloat16, scale_dtype=torch.float8_e8m0fnu, grad_f8=torch.float8_e4m3fn):
@@ -236,6 +236,9 @@ class RMMLinear8(RMMLinear):
     def _apply(self, fn, recurse=True):
         self._packed = None
         return super()._apply(fn, recurse)
+
+    def __getstate__(self):
+        return {**self.__dict__, "_packed": None}       # (a copy's weight is another, and counts its changes from zero)
 
     def pack(self):
         W = self.weight.detach()

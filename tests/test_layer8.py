@@ -1,5 +1,8 @@
 """CPU: RMMNorm and RMMLinear8 as modules, with stand-ins for the calls of the binding: plain numpy, so that neither a trace nor autograd
 sees into them, as with the kernels."""
+import copy
+import io
+
 import numpy as np
 import pytest
 import torch
@@ -191,3 +194,17 @@ def test_rows_with_another_kind_of_scales_are_refused_before_anything_happens(st
         with pytest.raises(TypeError, match="scale_dtype"):
             lin(rows)
     assert lin.calls == 0 and not stand_ins
+
+
+def test_copies_of_a_packed_layer_answer(stand_ins):
+    """A copy's weight counts its changes from zero: the packed form stays with the layer that made it."""
+    lin, X = layer(), torch.randn(5, 16)
+    with torch.no_grad():
+        want = lin.pack()(X)
+        file = io.BytesIO()
+        torch.save(lin, file)
+        file.seek(0)
+        for other in (copy.deepcopy(lin), copy.copy(lin), torch.load(file, weights_only=False)):
+            assert torch.equal(other(X), want)
+            other.weight.mul_(2), other.bias.zero_()
+            assert torch.equal(other.pack()(X), other(X))
