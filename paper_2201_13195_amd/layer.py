@@ -224,8 +224,9 @@ class RMMLinear8(RMMLinear):
     Rows8 of an RMMNorm in front of it.  `scale_dtype`: torch.float32, or torch.float8_e8m0fnu for powers of two;
     `grad_f8`: the format of dY's rows.
 
-    pack() keeps W's 8-bit form for calls without gradients, until W changes: such a call refuses then (a change through
-    weight.data, which torch does not count, goes unnoticed).  Copies of the layer, and what .to() makes of it, are not packed."""
+    pack() keeps W's 8-bit form for calls without gradients, until W changes: such a call refuses then (what torch does not count goes
+    unnoticed: a change through weight.data, or by a fused optimizer).  A forward pass that trains W, as it changes next, ends it; copies
+    of the layer, and what .to() makes of it, are not packed."""
 
     def __init__(self, in_features, out_features, bias=True, rho=0.1, k=None, kind=binding.GAUSSIAN, seed=0, layer_id=None,
                  device="cuda", dtype=torch.bfloat16, scale_dtype=torch.float8_e8m0fnu, grad_f8=torch.float8_e4m3fn):
@@ -279,6 +280,8 @@ class RMMLinear8(RMMLinear):
             X, data, scales = rows.Y, rows.data, rows.scales
         else:
             data = scales = None
+        if self.weight.requires_grad:
+            self.__dict__["_packed"] = None
         n = X.numel() // X.shape[-1]
         seed, offset = self.__dict__["last_state"] = self.next_state()
         return RMMLinear8Function.apply(X, data, scales, self.weight, self.bias, self.sketch_size(n), self.kind, seed, offset,

@@ -208,3 +208,23 @@ def test_copies_of_a_packed_layer_answer(stand_ins):
             assert torch.equal(other(X), want)
             other.weight.mul_(2), other.bias.zero_()
             assert torch.equal(other.pack()(X), other(X))
+
+
+def test_a_training_step_ends_the_packed_form(stand_ins):
+    """The fused optimizers change weights without counting it: after a forward pass that trains the weight nothing is answered from before."""
+    lin, X = layer(), torch.randn(5, 16)
+    opt = torch.optim.AdamW(lin.parameters(), lr=0.1, fused=True)
+    with torch.no_grad():
+        before = lin.pack()(X)
+    lin(X).sum().backward()
+    opt.step()
+    with torch.no_grad():
+        after = lin(X)
+        assert not torch.equal(after, before) and torch.allclose(after, X @ lin.weight.t() + lin.bias, atol=1e-5)
+        assert torch.equal(lin.pack()(X), after)
+    lin.weight.requires_grad_(False)
+    lin(X).sum().backward()
+    del stand_ins[:]
+    with torch.no_grad():
+        lin(X)
+    assert "quantize8_weight" not in stand_ins              # (a frozen weight stays packed)
