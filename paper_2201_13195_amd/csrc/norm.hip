@@ -68,25 +68,43 @@ __device__ __forceinline__ Rstd rstd_of(double sum, const NormArgs &g) {
 
 // Eight columns of y = h rstd w to 8 bits.  An 8-bit number is decided by where y / s lies between two of the format's, and
 // is as far off as they are apart where y is off by little and crosses over: y is made to twice the bits of fp32 here, as y + low, and
-// so is the largest magnitude, whose quotient is then rounded once.  A power of two takes y alone: its quotients are exact, and which
-// power it is does not hang on the last bits.
-template <int F8, int SCALE>
-__device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col, int lane, const float (&h)[8], const Rstd &r, const float (&w)[8]) {
+// so is the largest magnitude, whose quotient is then rounded once.  A power of two takes y alone, as its quotients are exact; which power
+// it is hangs on `low` where the largest magnitude lies one step of fp32 above top 2^k (top = 1.75 2^j): rounded to fp32 once, its quotient
+// is 2^k up to 0.875 of that step.
+struct Twice {
+    float y, low;
+};
+__device__ __forceinline__ Twice twice(float h, const Rstd &r, float w) {
 #pragma clang fp contract(off)  // (what a rounding left out would be counted twice where a sum takes the product whole)
+    const float p = h * r.high, p_low = fmaf(h, r.low, fmaf(h, r.high, -p));
+    const float v = p * w, v_low = fmaf(p_low, w, fmaf(p, w, -v)), y = v + v_low;
+    return {y, v_low - (y - v)};
+}
+template <typename T, int F8, int SCALE>
+__device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col, int lane, const float (&h)[8], const Rstd &r, const float (&w)[8]) {
     float y[8], low[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float p = h[i] * r.high, p_low = fmaf(h[i], r.low, fmaf(h[i], r.high, -p));
-        const float v = p * w[i], v_low = fmaf(p_low, w[i], fmaf(p, w[i], -v));
-        y[i] = v + v_low, low[i] = v_low - (y[i] - v);
+        const Twice t = twice(h[i], r, w[i]);
+        y[i] = t.y, low[i] = t.low;
     }
     const uint32_t most = max_of_16(amax8(y));
     const float amax = __uint_as_float(most);
     float q = amax / top_of<F8>();
-    if constexpr (SCALE == SCALE_F32) {
+    if (SCALE == SCALE_F32 || (most & 0x7FFFFFu) == 0x600001u) {  // (the same in the 16 lanes)
         float more = -INFINITY;  // of those as large in fp32, what is missing of the largest
 #pragma unroll
-        for (int i = 0; i < 8; ++i) more = magnitude(y[i]) == most ? fmaxf(more, y[i] < 0.0f ? -low[i] : low[i]) : more;
+        for (int i = 0; i < 8; ++i) {
+            Twice t = {y[i], low[i]};
+            // Made again for fp32 rows, whose registers are full: with powers of two 2048 x 16384 94 us, kept until here 99.  With the registers that
+            // this frees bf16 rows get a fifth wave a SIMD and are slower: 16384 x 4096 95, kept 92.
+            if constexpr (SCALE == SCALE_E8M0 && sizeof(T) == 4) {
+                float again = h[i];
+                asm("" : "+v"(again));
+                t = twice(again, r, w[i]);
+            }
+            more = magnitude(t.y) == most ? fmaxf(more, t.y < 0.0f ? -t.low : t.low) : more;
+        }
         q = fmaf(fmaf(-q, top_of<F8>(), amax) + max_of_16(more), 1.0f / top_of<F8>(), q);
     }
     const BlockScale s = block_scale<F8, SCALE>(q);
@@ -95,17 +113,18 @@ __device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col
         if ((lane & 15) == 0) store_scale<SCALE>(g.y8.scales, col / kBlock8 * g.y8.ld_scales + row, s);
     }
 }
+template <typename T>
 __device__ __forceinline__ void put8(const NormArgs &g, int64_t row, int64_t col, int lane, const float (&h)[8], const Rstd &r, const float (&w)[8]) {
     if (g.f8 == F8_E4M3) {
         if (g.scale == SCALE_F32)
-            put8<F8_E4M3, SCALE_F32>(g, row, col, lane, h, r, w);
+            put8<T, F8_E4M3, SCALE_F32>(g, row, col, lane, h, r, w);
         else
-            put8<F8_E4M3, SCALE_E8M0>(g, row, col, lane, h, r, w);
+            put8<T, F8_E4M3, SCALE_E8M0>(g, row, col, lane, h, r, w);
     } else {
         if (g.scale == SCALE_F32)
-            put8<F8_E5M2, SCALE_F32>(g, row, col, lane, h, r, w);
+            put8<T, F8_E5M2, SCALE_F32>(g, row, col, lane, h, r, w);
         else
-            put8<F8_E5M2, SCALE_E8M0>(g, row, col, lane, h, r, w);
+            put8<T, F8_E5M2, SCALE_E8M0>(g, row, col, lane, h, r, w);
     }
 }
 
@@ -152,7 +171,7 @@ __global__ void __launch_bounds__(Place<WPR>::THREADS) rms_norm_kernel(NormArgs 
             const int64_t col = p.col(c);
             float f[8];
             values<T, MODE>(w[c], col, g.d, f);
-            if (g.y8.data != nullptr) put8(g, row, col, p.lane, h[c], rstd, f);
+            if (g.y8.data != nullptr) put8<T>(g, row, col, p.lane, h[c], rstd, f);
             if (g.Y != nullptr) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * rstd.high * f[i];
@@ -193,7 +212,7 @@ __global__ void __launch_bounds__(1024) rms_norm_long_kernel(NormArgs g) {
             float w[8];
             take_h<T>(again, row, col, h);
             values<T, ROWS_RAGGED>(load_run<T, ROWS_RAGGED>((const T *)g.weight, col, g.d), col, g.d, w);
-            if (g.y8.data != nullptr) put8(g, row, col, p.lane, h, rstd, w);
+            if (g.y8.data != nullptr) put8<T>(g, row, col, p.lane, h, rstd, w);
             if (g.Y != nullptr) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[i] = h[i] * rstd.high * w[i];

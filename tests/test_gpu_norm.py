@@ -215,3 +215,27 @@ def test_long_matrix_passes_32_bit_offsets():
     dX, dw = rmm.rmm_rms_norm_backward(r.Y, X, w, r.rstd)
     dX3, _ = rmm.rmm_rms_norm_backward(few.Y, X[-3:].contiguous(), w, few.rstd)
     assert torch.equal(dX[-3:], dX3)
+
+
+@pytest.mark.parametrize("f8", eight.F8)
+def test_powers_of_two_at_the_border_between_two(f8):
+    """The largest magnitude of each block lies 0.55 to 0.85 steps of fp32 above the format's largest number: rounded by itself it is one
+    step above it and asks for the next power, but its quotient, rounded to fp32, is still 1 (up to 0.875 steps: half a step of 1)."""
+    d, top = 64 * 128, eight.TOP[f8]
+    X = torch.randn(1, d, generator=torch.Generator().manual_seed(11))
+    hat = X.double() / torch.sqrt((X.double() ** 2).mean() + EPS)
+    step = top * 2.0 ** -23 / 1.75                        # of fp32, at top = 1.75 * 2^k
+    weight = torch.ones(d)
+    for b in range(d // 128):
+        part = hat[0, b * 128:(b + 1) * 128].abs()
+        w = ((top + 0.7 * step) / part).float()
+        above = (part * w.double() - top) / step
+        fits = ((above > 0.55) & (above < 0.85) & (part > 0.1)).nonzero()
+        assert len(fits)
+        weight[b * 128 + int(fits[0])] = w[int(fits[0])]
+    y = (hat * weight.double()).view(-1, 128)
+    assert (y.abs().amax(1) > top).all() and (y.abs().amax(1).float() > top).all()
+    r = rmm.rmm_rms_norm(X.to(DEV), weight.to(DEV), None, EPS, need_Y=False, f8=f8, scale_dtype=torch.float8_e8m0fnu)
+    assert torch.equal((y.abs().amax(1) / top).float(), torch.ones(d // 128))
+    assert (eight.scale64(r.scales) == 1).all()
+    assert torch.equal(eight.bytes_of(r.Y8), eight.bytes_of(y.float().to(f8).view(1, d)))
