@@ -308,8 +308,8 @@ int rmm_linear8(int64_t n, int64_t d_in, int64_t d_out, int dtype, const rmm_mat
  *   H = X + residual, rounded to dtype (without a residual H is X and nothing is written)
  *   rstd_i = 1 / sqrt(mean_j H_ij^2 + eps)        Y_ij = H_ij rstd_i weight_j
  * with sums in 64 bits.  Outputs, each of which may be NULL: H (may be the buffer of X or of residual:
- * the update in place), Y (dtype), Y8 (8-bit rows of Y before its rounding, known to twice the bits of fp32), rstd[n] (fp32, for
- * the backward pass).  Y or Y8 must be asked for. */
+ * the update in place), Y (dtype), Y8 (8-bit rows of Y before its rounding, known to twice the bits of fp32
+ * where a row's root mean square lies between 2^-100 and 2^100), rstd[n] (fp32, for the backward pass).  Y or Y8 must be asked for. */
 int rmm_rms_norm(int64_t n, int64_t d, int dtype, float eps, const void *X, const void *residual, const void *weight,
                  void *H, void *Y, const rmm_mat8_t *Y8, float *rstd, void *stream);
 

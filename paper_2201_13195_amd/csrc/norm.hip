@@ -60,8 +60,11 @@ struct Rstd {
 __device__ __forceinline__ Rstd rstd_of(double sum, const NormArgs &g) {
     const double m = sum * g.inv_d + (double)g.eps;
     const double r = (double)(1.0f / sqrtf((float)m)), s = r * (1.5 - 0.5 * m * r * r);
-    // (where m is zero, infinite, no number or too far out for fp32, its own root says what fp32 makes of it)
-    if (!(m >= 0x1p-120 && m < 0x1p120)) return {(float)(1.0 / sqrt(m)), 0.0f};
+    // (where m is zero, infinite, no number or too far out for fp32, its own root says what fp32 makes of it; `low` where it has one)
+    if (!(m >= 0x1p-120 && m < 0x1p120)) {
+        const double x = 1.0 / sqrt(m);
+        return {(float)x, x >= 0x1p-124 && x < 0x1p127 ? (float)(x - (double)(float)x) : 0.0f};
+    }
     const float high = (float)s;
     return {high, (float)(s - (double)high)};
 }

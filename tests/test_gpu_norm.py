@@ -239,3 +239,22 @@ def test_powers_of_two_at_the_border_between_two(f8):
     assert torch.equal((y.abs().amax(1) / top).float(), torch.ones(d // 128))
     assert (eight.scale64(r.scales) == 1).all()
     assert torch.equal(eight.bytes_of(r.Y8), eight.bytes_of(y.float().to(f8).view(1, d)))
+
+
+@pytest.mark.parametrize("scale_dtype", eight.SCALES)
+@pytest.mark.parametrize("size,eps", [(1e25, EPS), (1e29, EPS), (1e-25, 0.0), (1e-29, 0.0)])
+def test_8_bit_rows_of_very_large_and_very_small_rows(size, eps, scale_dtype):
+    """Rows whose mean square is no number of fp32: scales and bytes are those of the result in 64 bits all the same."""
+    n, d, f8 = 60, 700, torch.float8_e4m3fn
+    X = torch.randn(n, d, generator=torch.Generator().manual_seed(12)) * size
+    w = 1 + 0.2 * torch.randn(d, generator=torch.Generator().manual_seed(13))
+    r = rmm.rmm_rms_norm(X.to(DEV), w.to(DEV), None, eps, need_Y=False, f8=f8, scale_dtype=scale_dtype)
+    y = X.double() / torch.sqrt((X.double() ** 2).mean(1, keepdim=True) + eps) * w.double()
+    y = torch.nn.functional.pad(y, (0, eight.blocks(d) * 128 - d)).view(n, -1, 128)
+    s = (y.abs().amax(2) / eight.TOP[f8]).float()
+    if scale_dtype == torch.float8_e8m0fnu:
+        m, e = torch.frexp(s)
+        s = torch.ldexp(torch.ones_like(s), torch.where(m == 0.5, e - 1, e))
+    assert torch.equal(eight.scale64(r.scales), s.t().double())
+    want = (y / s[..., None].double()).float().to(f8).view(n, -1)[:, :d]
+    assert torch.equal(eight.bytes_of(r.Y8), eight.bytes_of(want))
