@@ -96,7 +96,6 @@ __global__ void __launch_bounds__(64 * S::WAVES, 2) linear8_few_kernel(Linear8Ar
         for (int u = 0; u < TU; ++u)
 #pragma unroll
             for (int j = 0; j < TT; ++j) acc[u][j] = (f32x4_t){0, 0, 0, 0};
-        auto value = [](uint32_t s) { return SCALE == SCALE_F32 ? __uint_as_float(s) : e8m0_to_f32(s); };
         auto stored = [&](int i) -> uint32_t {
             if constexpr (SCALE == SCALE_F32)
                 return reinterpret_cast<const uint32_t *>(mine + S::TILES)[i];
@@ -115,14 +114,24 @@ __global__ void __launch_bounds__(64 * S::WAVES, 2) linear8_few_kernel(Linear8Ar
         for (int64_t b = wave; b < blocks; b += WAVES) {
             i32x8_t x[TT], w[TU];
             float s[TT];
+            [[maybe_unused]] uint32_t rest[SCALE == SCALE_F32 ? 1 : TT];
             wait_for_loads<0>();
 #pragma unroll
             for (int u = 0; u < TU; ++u) w[u] = fragment(TT + u);
 #pragma unroll
             for (int j = 0; j < TT; ++j) x[j] = fragment(j);
-            const float ws = value(stored(S::XS * 4 / S::SIZE + (SCALE == SCALE_F32 ? 0 : (int)((uint32_t)(w_scale + (uint64_t)b) & 3u))));
+            if constexpr (SCALE == SCALE_F32) {
+                const float ws = __uint_as_float(stored(S::XS));
 #pragma unroll
-            for (int j = 0; j < TT; ++j) s[j] = value(stored(16 * j + i16)) * ws;
+                for (int j = 0; j < TT; ++j) s[j] = __uint_as_float(stored(16 * j + i16)) * ws;
+            } else {
+                const uint32_t ws = stored(S::XS * 4 + (int)((uint32_t)(w_scale + (uint64_t)b) & 3u));
+#pragma unroll
+                for (int j = 0; j < TT; ++j) {
+                    const PowerProduct p = power_product(stored(16 * j + i16), ws);
+                    s[j] = p.s, rest[j] = p.rest;
+                }
+            }
             if (b + WAVES < blocks) {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the block has been read)
                 request(b + WAVES);
@@ -139,7 +148,7 @@ __global__ void __launch_bounds__(64 * S::WAVES, 2) linear8_few_kernel(Linear8Ar
 #pragma unroll
                 for (int j = 0; j < TT; ++j)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) xw[j][q] = widened<F8>(x[j], q);
+                    for (int q = 0; q < 4; ++q) xw[j][q] = widened<F8>(x[j], q, SCALE == SCALE_F32 ? 1.0f : __uint_as_float(rest[SCALE == SCALE_F32 ? 0 : j] << 23));
             }
 #pragma unroll
             for (int u = 0; u < TU; ++u) {
@@ -153,8 +162,10 @@ __global__ void __launch_bounds__(64 * S::WAVES, 2) linear8_few_kernel(Linear8Ar
                     f32x4_t part;
                     if constexpr (EXACT)
                         part = block_products(ww, xw[j]);
-                    else
+                    else if constexpr (SCALE == SCALE_F32)
                         part = block_products<F8>(w[u], x[j]);
+                    else
+                        part = block_products<F8>(w[u], x[j], rest[j]);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[u][j][r] = fmaf(part[r], s[j], acc[u][j][r]);
                 }

@@ -26,9 +26,16 @@ namespace {
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-// 2^(e - 127); 255 is no number.
-__device__ __forceinline__ float e8m0_to_f32(uint32_t e) {
-    return __uint_as_float(e == 255u ? 0x7FC00000u : e == 0u ? 0x00400000u : e << 23);
+// The product of two powers of two 2^(x - 127) and 2^(w - 127) (255: no number), whose exponents reach from -254 to 254, as s 2^(rest - 127)
+// with s among fp32's normal numbers.  `rest` goes to X's data, in front of the sum of a block: 127 nearly always, and what it is more or
+// less than that counts up to 64, as sums of a block (0, or 2^-25 to 2^32) times s are then infinite or nothing anyway.
+struct PowerProduct {
+    float s;
+    uint32_t rest;
+};
+__device__ __forceinline__ PowerProduct power_product(uint32_t x, uint32_t w) {
+    const int e = (int)(x + w) - 127, normal = min(max(e, 1), 254);
+    return {__uint_as_float(max(x, w) == 255u ? 0x7FC00000u : (uint32_t)normal << 23), (uint32_t)(min(max(e - normal, -64), 64) + 127)};
 }
 
 // The first `valid` bytes of 16, the others zero.
@@ -42,9 +49,9 @@ __device__ __forceinline__ uint4 first_bytes(uint4 q, int64_t valid) {
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// Bytes 8 q .. 8 q + 7 of a fragment as bf16 numbers.
+// Bytes 8 q .. 8 q + 7 of a fragment, times a power of two, as bf16 numbers.
 template <int F8>
-__device__ __forceinline__ bf16x8_t widened(const i32x8_t &f, int q) {
+__device__ __forceinline__ bf16x8_t widened(const i32x8_t &f, int q, float by = 1.0f) {
     union {
         bf16x8_t v;
         bf16x2_t p[4];
@@ -53,9 +60,9 @@ __device__ __forceinline__ bf16x8_t widened(const i32x8_t &f, int q) {
     for (int i = 0; i < 2; ++i) {
         const uint32_t u = (uint32_t)f[2 * q + i];
         if constexpr (F8 == F8_E4M3) {
-            o.p[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, false), o.p[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, true);
+            o.p[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, by, false), o.p[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, by, true);
         } else {
-            o.p[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(u, 1.0f, false), o.p[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(u, 1.0f, true);
+            o.p[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(u, by, false), o.p[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(u, by, true);
         }
     }
     return o.v;
@@ -65,6 +72,12 @@ template <int F8>
 __device__ __forceinline__ f32x4_t block_products(const i32x8_t &w, const i32x8_t &x) {
     const f32x4_t zero = {0, 0, 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, zero, 0, F8, 0, 0, 0, 0);
+}
+// The same with X times 2^(rest - 127).
+template <int F8>
+__device__ __forceinline__ f32x4_t block_products(const i32x8_t &w, const i32x8_t &x, uint32_t rest) {
+    const f32x4_t zero = {0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, zero, 0, F8, 0, 127, 0, (int)rest);
 }
 __device__ __forceinline__ f32x4_t block_products(const bf16x8_t (&w)[4], const bf16x8_t (&x)[4]) {
     f32x4_t part = {0, 0, 0, 0};

@@ -233,6 +233,7 @@ __global__ void __launch_bounds__(S::THREADS, 2) linear8_tile_kernel(Linear8Args
     constexpr int XS = SCALE == SCALE_F32 ? TJ : TJ / 4;
     uint32_t xs_read[XS], ws_read, xs[IN_MFMA ? XS : 1], ws = 0;
     float fs[IN_MFMA ? 1 : TJ];
+    [[maybe_unused]] float rest[SCALE == SCALE_E8M0 && EXACT ? TJ : 1];  // (a lane's fragments of X are of the tokens whose sums it holds)
     uint32_t w_byte = 0;  // address of the step's scale of W
     auto w_byte_of = [&](int64_t o0) { return (uint32_t)reinterpret_cast<uint64_t>(g.w.scales) + (uint32_t)((o0 + wo * S::WO) / kBlock8 * g.w.ld_scales) + group; };
     auto read_scales = [&] {
@@ -254,7 +255,10 @@ __global__ void __launch_bounds__(S::THREADS, 2) linear8_tile_kernel(Linear8Args
                 for (int q = 0; q < XS; ++q) xs[q] = xs_read[q];
             } else {
 #pragma unroll
-                for (int j = 0; j < TJ; ++j) fs[j] = e8m0_to_f32(xs_read[j / 4] >> (j % 4 * 8) & 255u) * e8m0_to_f32(w & 255u);
+                for (int j = 0; j < TJ; ++j) {
+                    const PowerProduct p = power_product(xs_read[j / 4] >> (j % 4 * 8) & 255u, w & 255u);
+                    fs[j] = p.s, rest[j] = __uint_as_float(p.rest << 23);
+                }
             }
         }
     };
@@ -316,7 +320,7 @@ __global__ void __launch_bounds__(S::THREADS, 2) linear8_tile_kernel(Linear8Args
 #pragma unroll
             for (int j = 0; j < TJ; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) xw[j][q] = widened<F8>(xf[j], q);
+                for (int q = 0; q < 4; ++q) xw[j][q] = widened<F8>(xf[j], q, SCALE == SCALE_F32 ? 1.0f : rest[SCALE == SCALE_F32 ? 0 : j]);
         }
         [[maybe_unused]] f32x4_t part[LATE + 1];
         for_each<S::MFMAS + (IN_MFMA ? 0 : LATE)>([&](auto index) __attribute__((always_inline)) {

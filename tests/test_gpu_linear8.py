@@ -292,3 +292,45 @@ def test_more_tiles_than_a_launch_has_work_groups():
         part = slice(at, min(at + 2048, n))
         want = rmm.rmm_linear8(X[part].view(E4), xs[:, part].view(torch.float8_e8m0fnu), *w)
         assert torch.equal(Y[part], want)
+
+
+def powers(n, d_in, d_out, X, W, f8, ex, ew):
+    """Operands with these data and powers of two: 2^(ex - 3 (b mod 4)) for X's block b, 2^(ew + 3 (b mod 4)) for W's."""
+    by = 3 * (torch.arange(eight.blocks(d_in)) % 4)
+
+    def pitched(A, f8):
+        a = torch.zeros(A.shape[0], (d_in + 15) // 16 * 16, dtype=torch.uint8)
+        a[:, :d_in] = A.to(f8).view(torch.uint8)
+        return a.to(DEV).view(f8)[:, :d_in]
+    xs = (127 + ex - by).to(torch.uint8)[:, None].expand(-1, (n + 15) // 16 * 16).contiguous()
+    ws = (127 + ew + by).to(torch.uint8)[None].expand(eight.blocks(d_out), -1).contiguous()
+    e8m0 = torch.float8_e8m0fnu
+    return (pitched(X, f8), xs.to(DEV).view(e8m0)[:, :n]), (pitched(W, E4), ws.to(DEV).view(e8m0))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,d_in,d_out", [shape for shape, _, _ in KERNELS])
+def test_scales_whose_product_is_no_number_of_fp32(n, d_in, d_out, dtype):
+    """Powers of two of both sides that multiply to more than fp32's largest number, or less than its smallest, where the result is one of
+    fp32's: with whole numbers it is exact, as no sum of up to 4 d_in of them needs more than 24 bits."""
+    g = torch.Generator().manual_seed(n + d_in)
+    for f8 in (E4, E5):
+        X, W = torch.randint(-2, 3, (n, d_in), generator=g).float(), torch.randint(-2, 3, (d_out, d_in), generator=g).float()
+        # 2^-18 of whole numbers up to 4 d_in <= 2^15, times 2^130
+        x, w = powers(n, d_in, d_out, X * 2.0 ** -9, W * 2.0 ** -9, f8, 100, 30)
+        want = eight.values_rows(*x) @ eight.values_weight(*w).t()
+        assert torch.equal(rmm.rmm_linear8(*x, *w, dtype=dtype).cpu(), want.to(dtype))
+        # zeros stay zeros, whatever the scales
+        x, w = powers(n, d_in, d_out, torch.zeros(n, d_in), W, f8, 120, 110)
+        assert (rmm.rmm_linear8(*x, *w, dtype=dtype) == 0).all()
+        # 384^2 and more for each product, times 2^-150: a block's sum of 128 is one of fp32's normal numbers
+        X, W = 448 - 32 * torch.randint(0, 2, (n, d_in), generator=g).float(), 448 - 32 * torch.randint(0, 3, (d_out, d_in), generator=g).float()
+        x, w = powers(n, d_in, d_out, X, W, f8, -90, -60)
+        X64, W64 = eight.values_rows(*x), eight.values_weight(*w)
+        Y = rmm.rmm_linear8(*x, *w, dtype=dtype).cpu().double()
+        want = X64 @ W64.t()
+        # (the sum as in `check`; a last block of fewer may be less than 2^-126, and lost)
+        bound = (d_in + 4) * 2.0 ** -23 * want + eight.HALF[dtype] * want * (1 + 2.0 ** -8) + 2.0 ** -126
+        if dtype == torch.bfloat16:
+            bound += 7 * 2.0 ** -13 * want
+        assert ((Y - want).abs() <= bound).all(), float(((Y - want).abs() / bound).max())
