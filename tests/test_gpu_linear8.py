@@ -334,3 +334,34 @@ def test_scales_whose_product_is_no_number_of_fp32(n, d_in, d_out, dtype):
         if dtype == torch.bfloat16:
             bound += 7 * 2.0 ** -13 * want
         assert ((Y - want).abs() <= bound).all(), float(((Y - want).abs() / bound).max())
+
+
+@pytest.mark.parametrize("scale_dtype", eight.SCALES)
+@pytest.mark.parametrize("n,d_in,d_out", [shape for shape, _, _ in KERNELS])
+def test_fp32_results_hold_what_stands_beside_a_large_product(n, d_in, d_out, scale_dtype):
+    """One product of 2^15 in each eight contraction elements, the others 1, -1 or 0: the 8-bit matrix instruction would cut those off.
+    No sum needs more than 24 bits, so the result is exact."""
+    g = torch.Generator().manual_seed(n + d_out)
+    for f8 in (E4, E5):
+        X, W = torch.randint(-1, 2, (n, d_in), generator=g).float(), torch.randint(-1, 2, (d_out, d_in), generator=g).float()
+        at = torch.arange(0, d_in - 7, 8) + torch.randint(0, 8, (d_in // 8,), generator=g)
+        X[:, at], W[:, at] = X[:, at] * 256, W[:, at] * 128
+        x, w = powers(n, d_in, d_out, X, W, f8, 3, -3)
+        if scale_dtype == torch.float32:
+            xs = torch.zeros(x[1].shape[0], x[1].stride(0), device=DEV)
+            xs[:, :n] = x[1].float()
+            x, w = (x[0], xs[:, :n]), (w[0], w[1].float())
+        want = eight.values_rows(*x) @ eight.values_weight(*w).t()
+        assert torch.equal(rmm.rmm_linear8(*x, *w, dtype=torch.float32).cpu().double(), want)
+
+
+@pytest.mark.parametrize("scale_dtype", eight.SCALES)
+@pytest.mark.parametrize("n,d_in,d_out", [shape for shape, _, _ in KERNELS])
+def test_fp32_results_in_the_mean(n, d_in, d_out, scale_dtype):
+    """The roundings of d_in sums, and of four more for scales and product, are independent: each at most 2^-23 of a partial sum, which for
+    products of both signs is no more than the root of the sum of their squares in the mean."""
+    for f8 in (E4, E5):
+        x, w, _ = operands(n, d_in, d_out, f8, scale_dtype)
+        X, W = eight.values_rows(*x).to(DEV), eight.values_weight(*w).to(DEV)
+        off = rmm.rmm_linear8(*x, *w, dtype=torch.float32).double() - X @ W.t()
+        assert float(off.norm()) <= (d_in + 4) ** 0.5 * 2.0 ** -23 * float((X.square() @ W.square().t()).sum().sqrt())

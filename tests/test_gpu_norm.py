@@ -258,3 +258,27 @@ def test_8_bit_rows_of_very_large_and_very_small_rows(size, eps, scale_dtype):
     assert torch.equal(eight.scale64(r.scales), s.t().double())
     want = (y / s[..., None].double()).float().to(f8).view(n, -1)[:, :d]
     assert torch.equal(eight.bytes_of(r.Y8), eight.bytes_of(want))
+
+
+@pytest.mark.parametrize("n,d,dtype", [((1 << 31) // 2048 + 5, 2048, torch.bfloat16), (300001, 257, torch.float32), (60000, 5000, torch.bfloat16),
+                                       (6001, 20000, torch.float32), (30000, 16392, torch.bfloat16)])
+def test_weight_gradient_of_many_rows(n, d, dtype):
+    """A thread adds at most n / 64 rows (long rows; n / 256 others), and up to 512 such sums follow.  The roundings are independent, each at
+    most 2^-24 of a partial sum, which in the mean is no more than the root of the sum of squares; eight more for what is summed."""
+    g = torch.Generator(DEV).manual_seed(n)
+    X = torch.empty(n, d, dtype=dtype, device=DEV)
+    dY = torch.empty(n, d, dtype=dtype, device=DEV)
+    for t in (X, dY):
+        t.normal_(generator=g)
+    w = torch.ones(d, dtype=dtype, device=DEV)
+    rstd = rmm.rmm_rms_norm(X, w, None, EPS).rstd
+    _, dw = rmm.rmm_rms_norm_backward(dY, X, w, rstd, need_dX=False)
+    want, squares = torch.zeros(d, dtype=torch.float64, device=DEV), torch.zeros(d, dtype=torch.float64, device=DEV)
+    for at in range(0, n, 1 << 14):
+        h, dy = X[at:at + (1 << 14)].double(), dY[at:at + (1 << 14)].double()
+        part = dy * h / torch.sqrt((h * h).mean(1, keepdim=True) + EPS)
+        want += part.sum(0)
+        squares += part.square().sum(0)
+    adds = n / (64 if d > 16384 else 256) + 512
+    off = float((dw.double() - want).norm())
+    assert off <= (adds ** 0.5 + 8) * STEP * float(squares.sum().sqrt()) + 1.01 * eight.HALF[dtype] * float(want.norm())
