@@ -24,8 +24,10 @@ enum {
 //   - the smallest FEW kernel with no more work-groups than compute units: its time is one round of a latency and the contraction.
 //       24 x 4096 -> 1024 16x16 4.3, 16x32 4.5, 128 x 128 tiles 20;   128 x 768 -> 768 16x16 3.9 (384 work-groups), 16x32 3.4, 32x32 3.8;
 //       64 x 4096 -> 4096 16x32 8.7 (512), 32x32 7.0, 64x32 7.5;   128 x 4096 -> 4096 32x32 10.1 (512), 64x32 8.0, MANY 32x32 8.8
-//   - instead of 64x32 MANY 32x32, two work-groups to a compute unit, where its four waves have no more than two blocks each:
-//       333 x 1000 -> 1111 4.8 (64x32 5.1);   fp32 results 5.1 (5.5)
+//   - instead of 64x32 MANY 32x32, two work-groups to a compute unit, where its four waves have no more than two blocks each (traced
+//     launches, fp32 scales, 64x32 in brackets):  128 x 256 -> 4096 4.2 (4.5), 1000 x 256 -> 400 4.3 (4.5), 500 x 384 -> 900 4.4 (4.6),
+//       64 x 512 -> 6000 4.4 (4.6), 200 x 512 -> 2048 4.4 (4.7), 2000 x 640 -> 256 4.7 (5.1), 256 x 768 -> 2048 4.8 (5.0), 400 x 900 -> 1000 5.3 (5.7),
+//       500 x 1024 -> 768 5.0 (5.1), 128 x 1024 -> 4000 5.3 (5.3);   twelve blocks:  200 x 1536 -> 2048 5.8 (5.6), 500 x 1536 -> 768 5.7 (5.5)
 //   - up to 64 tokens and more outputs than that: the weights are read once, whatever the tile, and four waves of more outputs keep more of
 //     them in flight.  1 x 4096 -> 32000 (131 MB) 16x32 23.9, MANY 16x64 20.2, 128 x 128 tiles 27.9;  32 x 4096 -> 16384 MANY 32x32 12.8,
 //     64x32 13.5, 64 x 128 tiles 15.1;  48 x 4096 -> 16384 MANY 32x32 20.8, 64x32 14.1, 64 x 128 tiles 15.6
@@ -35,9 +37,16 @@ enum {
 //     64 x 128 from six blocks of it on (three for fp32 results, whose every block is four times the work), 128 x 128 from twenty.
 //       512 x 4096 -> 4096 64 x 128 16.9, 128 x 128 split 22.0, as below 26.6;   512 x 1024 -> 4096 8.1, 9.3, 8.6;   512 x 640 -> 4096 7.3, 8.5, 7.1;
 //       1024 x 4096 -> 4096 (512 of 64 x 128) 31.4, 25.1, 28.9;   1024 x 2560 -> 4096 22.9, 17.3, 18.3;   1024 x 2048 -> 4096 20.1, 14.6, 14.6
-//   - as many as there are, one group of waves each.  A 256 x 256 tile is 1.2 us a step of 128 and 3 us of its own, with a compute unit
-//     to itself; two 128 x 128 tiles share one, 0.95 us a step of both and 2 us:  8192 x 1024 -> 1024 256 18.8, 128 14.5;  4096 x 1024 -> 4096 256 21.8, 128 24.5;
-//     16384 x 4096 -> 4096 256 207, 128 255.  fp32 results have no 256 x 256 tiles (the exact way needs the registers).
+//   - as many as there are, one group of waves each.  A 256 x 256 tile has a compute unit to itself, two 128 x 128 tiles share one.  The model
+//     below counts, in hundredths of us, 1.2 us for a step of 128 (0.95 for both small ones) and 3 (2) more for a round of tiles. Measured, a step
+//     of the large tile is 1.3 to 1.5 up to 16 of them and 1.6 beyond (8192 x 1024, 2048, 4096 -> 2048, one round: 22.2, 34.1, 59.8), so that
+//     near the break-even the large tile is taken where the small one would do better (bf16 results, fp32 scales, the same operands again and again):
+//       256 taken:  4096 x 1024 -> 4096 256 21.9, 128 23.9;   8192 x 512 -> 4096 25.7, 27.3;   8192 x 1024 -> 2048 22.2, 23.9;   16384 x 1024 -> 1024 22.4, 24.0;
+//         7000 x 2048 -> 4096 59.5, 67.1;   16384 x 1024 -> 4096 72, 85;   8192 x 4096 -> 4096 115, 143;   16384 x 4096 -> 4096 225, 282 (powers of two 211, 262)
+//       256 taken, and 128 would be faster:  16384 x 768 -> 768 17.5, 17.1;   4096 x 1024 -> 2560 19.2, 18.9;   6000 x 1024 -> 4096 34.4, 33.8;
+//         3000 x 1500 -> 6000 48.3, 43.0;   5000 x 1024 -> 4096 33.1, 29.0
+//       128 taken:  8192 x 1024 -> 1024 18.7, 14.1;   4096 x 2048 -> 2048 28.6, 22.1
+//     fp32 results have no 256 x 256 tiles (the exact way needs the registers).
 inline int64_t linear8_groups(int64_t n, int64_t d_out, int64_t tokens, int64_t outputs) {
     return ((n + tokens - 1) / tokens) * ((d_out + outputs - 1) / outputs);
 }

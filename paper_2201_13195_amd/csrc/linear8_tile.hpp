@@ -35,13 +35,13 @@ __device__ __forceinline__ void for_each(F f) {
 // BT x BO outputs on NT x NO waves.  PD fragments of W are read ahead, so that the one barrier of a step stands PD fragments before
 // its end, and the loads of the step that is STAGES ahead, into the stage that is free then, have STAGES - 1 steps to arrive.  They are
 // spread over the MFMAs behind the barrier.  KS groups of such waves share the contraction, every KS-th step a group's; each has stages of
-// its own, and the barrier is one for all.  Measured beside what is below, bf16 results, in us:
+// its own, and the barrier is one for all.  Measured beside what is below, bf16 results, the same operands again and again, in us:
 //   - 128 x 128 tiles, four stages and one group: 1024 x 4096 -> 4096 with powers of two 23.8, with fp32 scales 25.9 (two groups of two
 //     stages 24.8, 24.9); one group leaves a SIMD one wave, whose reads nothing hides
 //   - 64 x 128 tiles, two groups of two stages: 512 x 4096 -> 4096 19.5 (three stages 16.9); one group of five 21.8
 //   - a second barrier, behind which half of a 256 x 256 tile's loads have half a step more: 16384 x 4096 -> 4096 with powers of two
 //     217 -> 212, with fp32 scales 228 -> 236
-//   - every other tile backwards along the contraction: 207 -> 209
+//   - every other tile backwards along the contraction: 16384 x 4096 -> 4096 with powers of two 207 -> 209
 template <int BT_, int BO_, int NT_, int NO_, int KS_, int STAGES_>
 struct Tile8 {
     static constexpr int BT = BT_, BO = BO_, NT = NT_, NO = NO_, KS = KS_, STAGES = STAGES_, PD = 3;
