@@ -247,9 +247,10 @@ class RMMLinear8(RMMLinear):
         return self
 
     def _weight8(self, W):
-        if self._packed is None:
+        packed = self._packed                    # (once: a training call in another thread may end it)
+        if packed is None:
             return binding.rmm_quantize8_weight(_dense(W.detach()), scale_dtype=self.scale_dtype)
-        w8, of, version = self._packed
+        w8, of, version = packed
         if of is not self.weight or version != self.weight._version:
             raise RuntimeError("RMMLinear8: the weight has changed since pack(); call pack() again")
         return w8

@@ -228,3 +228,19 @@ def test_a_training_step_ends_the_packed_form(stand_ins):
     with torch.no_grad():
         lin(X)
     assert "quantize8_weight" not in stand_ins              # (a frozen weight stays packed)
+
+
+def test_a_packed_form_that_ends_under_a_call(stand_ins):
+    """Another thread's training call may end it at any moment: a call that has begun goes on with what it has read."""
+    class Ends(rmm.RMMLinear8):
+        def __getattribute__(self, name):
+            value = super().__getattribute__(name)
+            if name == "_packed" and value is not None:
+                self.__dict__["_packed"] = None             # as if by another thread, right behind the read
+            return value
+
+    lin, X = layer(), torch.randn(5, 16)
+    with torch.no_grad():
+        want = lin.pack()(X)
+        lin.__class__ = Ends
+        assert torch.equal(lin(X), want) and torch.equal(lin(X), want)
